@@ -285,6 +285,54 @@ ec_status ec_validate_routing(const ec_config* cfg, const int32_t* I, const int3
                               const int32_t* slots, int64_t* violations, void* ws, size_t ws_bytes,
                               void* cuda_stream);
 
+/*
+ * Tokens sorted by expert and back (the paper has no counterpart beyond Section 3.1's contrast: token choice as it is trained
+ * and served where no request is dropped).  Every token names `per_token` experts; the rows of an expert are the tokens
+ * that named it, as many as they are, one expert after the other.  For callers that run experts of their own on those rows, and
+ * for ec_mx_expert_gemm below.
+ *   choice  [n, per_token]  int32, the experts of each token; an entry outside [0, E) names none (a padded token, a dropped
+ *                           request).  A token may name an expert twice; that is two rows.
+ *   offsets [E + 1]         int32, expert e's rows are offsets[e] .. offsets[e + 1] - 1; offsets[E] = m rows in all
+ *   order   [n * per_token] int32, row r < m holds flat choice order[r] = t * per_token + j (token t), ascending inside an expert;
+ *                           entries from m on are left as they were
+ *   place   [n, per_token]  int32, the row of each choice, -1 where it names no expert: the inverse of `order`
+ * Row matrices (X_s, Y, dY) have n * per_token rows, of which the first m are read and written; the others are left as they were.
+ * X, X_out, dX_out and X_s have the element type cfg->dtype, Y and dY cfg->y_dtype, weights and dweights are fp32.
+ * Restrictions (EC_ERR_UNSUPPORTED): rows of d_model elements of either type a multiple of 16 bytes, d_model <= 2^22 - 64,
+ * 1 <= E <= 256, 1 <= per_token <= 32, n * per_token < 2^31.  n = 0 is a call: it writes offsets (zeros) and
+ * nothing else, and its empty arguments may be NULL.  An output must not overlap an input or another output.  Any contents of
+ * `choice` and of `place` are safe to pass: what lies outside its range counts as "no expert".
+ */
+typedef struct {
+  int64_t n;         /* tokens                                                            */
+  int32_t d_model;   /* d                                                                 */
+  int32_t E;         /* number of experts                                                 */
+  int32_t per_token; /* choices per token                                                 */
+  int32_t dtype;     /* ec_dtype of X, X_out, X_s                                         */
+  int32_t y_dtype;   /* ec_dtype of Y, dY; EC_BF16 only with dtype = EC_BF16              */
+} ec_sort_config;
+
+/* Bytes of scratch ec_sort_tokens needs, 256-byte aligned (at most 256 KiB).  0 on a bad cfg. */
+size_t ec_sort_workspace_bytes(const ec_sort_config* cfg);
+
+/* The plan: offsets, order and place of `choice`.  Counting and ranking only, no atomics on global memory: the result is unique.
+ * One launch up to 16384 choices, two beyond. */
+ec_status ec_sort_tokens(const ec_sort_config* cfg, const int32_t* choice, int32_t* offsets, int32_t* order, int32_t* place,
+                         void* ws, size_t ws_bytes, void* cuda_stream);
+
+/* X_s[place[t, j], :] = X[t, :] for every choice that names an expert.  Its gradient is ec_combine with weights = NULL. */
+ec_status ec_dispatch(const ec_sort_config* cfg, const void* X, const int32_t* place, void* X_s, void* cuda_stream);
+
+/* X_out[t, :] = sum over j of weights[t, j] * Y[place[t, j], :], j ascending, accumulated in fp32 and rounded once; choices
+ * without a row add nothing (whatever their weight holds), a token without any has a zero row.  weights = NULL: all ones. */
+ec_status ec_combine(const ec_sort_config* cfg, const void* Y, const float* weights, const int32_t* place, void* X_out,
+                     void* cuda_stream);
+
+/* Gradient of ec_combine: dY[place[t, j], :] = weights[t, j] * dX_out[t, :] and dweights[t, j] = <dX_out[t, :], Y[place[t, j], :]>
+ * (fp32, in a fixed order; 0 for a choice without a row). */
+ec_status ec_combine_backward(const ec_sort_config* cfg, const void* dX_out, const void* Y, const float* weights,
+                              const int32_t* place, void* dY, float* dweights, void* cuda_stream);
+
 /* 1 if this library was built with -DEC_DEBUG: every kernel then range-checks each index it reads from I, row_ptr
  * or slots before using it, skips the access when it is out of range and records EC_ERR_INDEX in the status word
  * (ec_read_status).  The normal build compiles these checks out. */

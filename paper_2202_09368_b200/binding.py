@@ -26,7 +26,8 @@ EXPORTS = ["ec_capacity", "ec_workspace_bytes", "ec_saved_bytes", "ec_saved_view
            "ec_moe_forward", "ec_moe_backward", "ec_read_status", "ec_status_string",
            "ec_uses_tensor_cores", "ec_launch_count", "ec_profile_enable", "ec_profile_read",
            "ec_route_static", "ec_route_static_bytes", "ec_shuffle", "ec_unshuffle",
-           "ec_forward_only_workspace_bytes", "ec_capped_assignment", "ec_route_token_choice", "ec_expert_gemm", "ec_validate_routing", "ec_debug_build", "ec_backward_view"]
+           "ec_forward_only_workspace_bytes", "ec_capped_assignment", "ec_route_token_choice", "ec_expert_gemm", "ec_validate_routing", "ec_debug_build", "ec_backward_view",
+           "ec_sort_workspace_bytes", "ec_sort_tokens", "ec_dispatch", "ec_combine", "ec_combine_backward"]
 EC_GEMM_XW1, EC_GEMM_HW2T, EC_GEMM_ATB = 0, 1, 2
 EC_ROUTE_STATIC_SCRATCH_BYTES = 8 << 20
 
@@ -45,6 +46,11 @@ class ec_saved_ptrs(C.Structure):
 
 class ec_backward_ptrs(C.Structure):
     _fields_ = [(name, C.c_void_p) for name in ("dX_e", "dG", "dZ", "dX_in", "dL")] + [("dL_is_bf16", C.c_int32)]
+
+
+class ec_sort_config(C.Structure):
+    _fields_ = [("n", C.c_int64), ("d_model", C.c_int32), ("E", C.c_int32), ("per_token", C.c_int32), ("dtype", C.c_int32),
+                ("y_dtype", C.c_int32)]
 
 
 class EcError(RuntimeError):
@@ -94,6 +100,12 @@ def lib():
         L.ec_profile_enable.restype = None; L.ec_profile_enable.argtypes = [C.c_int]
         L.ec_profile_read.restype = C.c_int
         L.ec_profile_read.argtypes = [C.POINTER(C.c_float), C.POINTER(C.c_char_p), C.c_int]
+        Q = C.POINTER(ec_sort_config)
+        L.ec_sort_workspace_bytes.restype = C.c_size_t; L.ec_sort_workspace_bytes.argtypes = [Q]
+        L.ec_sort_tokens.restype = C.c_int; L.ec_sort_tokens.argtypes = [Q, V, V, V, V, V, C.c_size_t, V]
+        L.ec_dispatch.restype = C.c_int; L.ec_dispatch.argtypes = [Q, V, V, V, V]
+        L.ec_combine.restype = C.c_int; L.ec_combine.argtypes = [Q, V, V, V, V, V]
+        L.ec_combine_backward.restype = C.c_int; L.ec_combine_backward.argtypes = [Q, V, V, V, V, V, V, V]
         _lib = L
     return _lib
 
@@ -253,6 +265,94 @@ def ec_expert_gemm(cfg, kind, A, Bm, out=None, ws=None):
     _check(lib().ec_expert_gemm(C.byref(cfg), kind, _ptr(A), _ptr(Bm), _ptr(out), _ptr(ws), ws.numel(), _stream()),
            "ec_expert_gemm")
     return out
+
+
+# ---- tokens sorted by expert ------------------------------------------------------------------------------------------------
+
+def make_sort_config(n, d_model, E, per_token, dtype=torch.float32, y_dtype=None) -> ec_sort_config:
+    """n tokens that name per_token experts each.  dtype: of X, X_out, X_s; y_dtype: of Y, dY (None: the same)."""
+    types = {torch.float32: EC_F32, torch.bfloat16: EC_BF16}
+    return ec_sort_config(int(n), int(d_model), int(E), int(per_token), types[dtype], types[dtype if y_dtype is None else y_dtype])
+
+
+def ec_sort_workspace_bytes(cfg: ec_sort_config) -> int:
+    return int(lib().ec_sort_workspace_bytes(C.byref(cfg)))
+
+
+_TYPES = {EC_F32: torch.float32, EC_BF16: torch.bfloat16}
+
+
+def _dense(what, dev, *tensors):
+    """The operands of one of the calls below: dense device tensors of one device, each (tensor, dtype, shape).  The library sees addresses
+    only, so what is not like this is refused here.  Returns their addresses."""
+    out = []
+    for t, dtype, shape in tensors:
+        if t.dtype is not dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
+            raise EcError(EC_ERR_INVALID_ARG, f"{what}: wanted a dense {dtype} tensor {tuple(shape)} on {dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        out.append(t.data_ptr())
+    return out
+
+
+def _stream_of(what, dev):
+    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
+        raise EcError(EC_ERR_INVALID_ARG, f"{what}: the operands are on {dev}, which is not the current CUDA device")
+    return torch._C._cuda_getCurrentRawStream(dev.index)
+
+
+@dataclass
+class Sorted:
+    offsets: torch.Tensor      # [E + 1] first row of each expert, rows in all
+    order: torch.Tensor        # [n * per_token] the flat choice of each row
+    place: torch.Tensor        # [n, per_token] the row of each choice, -1: none
+
+
+def ec_sort_tokens(cfg, choice, out: Sorted | None = None, ws=None) -> Sorted:
+    """The plan of a dropless token-choice layer: choice [n, per_token] int32 holds each token's experts (outside [0, E): none)."""
+    dev, n, K, E = choice.device, cfg.n, cfg.per_token, cfg.E
+    stream = _stream_of("ec_sort_tokens", dev)
+    if out is None:
+        out = Sorted(torch.empty(E + 1, dtype=torch.int32, device=dev), torch.empty(n * K, dtype=torch.int32, device=dev),
+                     torch.empty(n, K, dtype=torch.int32, device=dev))
+    if ws is None:
+        ws = torch.empty(ec_sort_workspace_bytes(cfg), dtype=torch.uint8, device=dev)
+    i32 = torch.int32
+    c, o, r, p, w = _dense("ec_sort_tokens", dev, (choice, i32, (n, K)), (out.offsets, i32, (E + 1,)), (out.order, i32, (n * K,)),
+                           (out.place, i32, (n, K)), (ws, torch.uint8, ws.shape))
+    _check(lib().ec_sort_tokens(C.byref(cfg), c, o, r, p, w, ws.numel(), stream), "ec_sort_tokens")
+    return out
+
+
+def ec_dispatch(cfg, X, place, X_s=None):
+    """X_s[place[t, j], :] = X[t, :]; rows of X_s that no choice holds are left as they were.  Gradient: ec_combine(cfg, dX_s, None, place)."""
+    dev, n, K, d, dt = X.device, cfg.n, cfg.per_token, cfg.d_model, _TYPES[cfg.dtype]
+    stream = _stream_of("ec_dispatch", dev)
+    X_s = torch.empty(n * K, d, dtype=dt, device=dev) if X_s is None else X_s
+    x, p, s = _dense("ec_dispatch", dev, (X, dt, (n, d)), (place, torch.int32, (n, K)), (X_s, dt, (n * K, d)))
+    _check(lib().ec_dispatch(C.byref(cfg), x, p, s, stream), "ec_dispatch")
+    return X_s
+
+
+def ec_combine(cfg, Y, weights, place, X_out=None):
+    """X_out[t, :] = sum_j weights[t, j] * Y[place[t, j], :]; weights None: all ones."""
+    dev, n, K, d, dt = Y.device, cfg.n, cfg.per_token, cfg.d_model, _TYPES[cfg.dtype]
+    stream = _stream_of("ec_combine", dev)
+    X_out = torch.empty(n, d, dtype=dt, device=dev) if X_out is None else X_out
+    y, p, x = _dense("ec_combine", dev, (Y, _TYPES[cfg.y_dtype], (n * K, d)), (place, torch.int32, (n, K)), (X_out, dt, (n, d)))
+    w = None if weights is None else _dense("ec_combine", dev, (weights, torch.float32, (n, K)))[0]
+    _check(lib().ec_combine(C.byref(cfg), y, w, p, x, stream), "ec_combine")
+    return X_out
+
+
+def ec_combine_backward(cfg, dX_out, Y, weights, place, dY=None, dweights=None):
+    """Gradients of ec_combine: (dY [n * per_token, d], rows that no choice holds left as they were; dweights [n, per_token] fp32)."""
+    dev, n, K, d, ty = Y.device, cfg.n, cfg.per_token, cfg.d_model, _TYPES[cfg.y_dtype]
+    stream = _stream_of("ec_combine_backward", dev)
+    dY = torch.empty(n * K, d, dtype=ty, device=dev) if dY is None else dY
+    dweights = torch.empty(n, K, dtype=torch.float32, device=dev) if dweights is None else dweights
+    g, y, w, p, dy, dw = _dense("ec_combine_backward", dev, (dX_out, _TYPES[cfg.dtype], (n, d)), (Y, ty, (n * K, d)), (weights, torch.float32, (n, K)),
+                                (place, torch.int32, (n, K)), (dY, ty, (n * K, d)), (dweights, torch.float32, (n, K)))
+    _check(lib().ec_combine_backward(C.byref(cfg), g, y, w, p, dy, dw, stream), "ec_combine_backward")
+    return dY, dweights
 
 
 def ec_validate_routing(cfg, I, row_ptr, slots, ws=None) -> int:

@@ -173,6 +173,17 @@ cudaError_t launch_capped_assignment(const float* S, int64_t ng, int E, int64_t 
 cudaError_t launch_gather_gate(const float* S, const int32_t* I, float* G, int64_t slots_total, int64_t k, int E,
                                int64_t n, int* status, cudaStream_t st);
 
+// ---- tokens sorted by expert (sorted.cu) ---------------------------------------------------------
+// total = n * per_token flat choices; scratch as sort_scratch_bytes says
+size_t sort_scratch_bytes(int E);
+cudaError_t launch_sort_tokens(const int32_t* choice, int64_t total, int E, int32_t* offsets, int32_t* order, int32_t* place,
+                               void* scratch, cudaStream_t st);
+cudaError_t launch_dispatch(const void* X, const int32_t* place, void* X_s, int64_t n, int64_t row_bytes, int K, cudaStream_t st);
+cudaError_t launch_combine_rows(int dtype, int y_dtype, const void* Y, const float* weights, const int32_t* place, void* X_out,
+                                int64_t n, int d, int K, cudaStream_t st);
+cudaError_t launch_combine_backward(int dtype, int y_dtype, const void* dX_out, const void* Y, const float* weights,
+                                    const int32_t* place, void* dY, float* dweights, int64_t n, int d, int K, cudaStream_t st);
+
 // ---- plain FMA GEMM (gemm_simt.cu) -------------------------------------------------------------
 enum Epilogue { EPI_STORE = 0, EPI_GELU = 1, EPI_GELU_GRAD = 2, EPI_ADD_SLOTS = 3 };
 

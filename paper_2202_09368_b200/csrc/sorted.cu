@@ -1,0 +1,405 @@
+// Tokens sorted by expert and back: the plan (a stable counting sort of the choices), the dispatch of rows, the weighted
+// combine and its gradient.  All of it moves memory: the floor of each call is its bytes at the copy rate.
+#include "internal.h"
+
+#include <limits.h>
+
+namespace ecmoe {
+
+namespace {
+
+// ---- the plan ----------------------------------------------------------------------------------------------
+// A counting sort.  The flat choices are cut into one contiguous piece per CTA and those into one per warp; a choice's row is
+//   offsets[e] + (choices of e in earlier CTAs) + (in earlier warps of this CTA) + (earlier in this warp),
+// all of them plain counts, so the order is the stable one and unique.  A warp counts 32 choices at a time: the lanes with the
+// same expert find each other (match), the lowest adds their number to the warp's own row of counters in shared memory.
+// Up to kOnePiece choices one CTA does it all; beyond, a first launch leaves every CTA's counts and in the second each CTA sums
+// what it needs of them (148 x 256 counters at most, 148 KiB out of L2).
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kMaxExperts = 256;
+constexpr int64_t kOnePiece = 16384;
+constexpr int kMaxPieces = 148;
+
+struct SortArgs {
+  const int32_t* choice; int32_t* offsets; int32_t* order; int32_t* place; int* counts;   // counts [pieces, E]
+  int64_t total, per_cta;                                                                  // flat choices; per_cta a multiple of 1024
+  int E, pieces;
+};
+
+// counts of one warp's stretch [lo, hi) into mine[0 .. E)
+__device__ __forceinline__ void count_stretch(const int32_t* choice, int64_t lo, int64_t hi, int E, int* mine, int lane) {
+  constexpr int U = 8;                                  // choices on their way per lane
+  for (int64_t i = lo; i < hi; i += 32 * U) {
+    int e[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) { const int64_t at = i + 32 * u + lane; e[u] = at < hi ? __ldg(choice + at) : -1; }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool in = (unsigned)e[u] < (unsigned)E;
+      const unsigned peers = __match_any_sync(0xffffffffu, in ? e[u] : -1);
+      if (in && (peers & ((1u << lane) - 1)) == 0) mine[e[u]] += __popc(peers);
+      __syncwarp();
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs a) {
+  __shared__ int counters[kSortWarps][kMaxExperts];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int e = lane; e < a.E; e += 32) counters[warp][e] = 0;
+  __syncwarp();
+  chain_enter();
+  const int32_t* choice = after_enter(a.choice);
+  const int64_t per_warp = a.per_cta / kSortWarps, lo = blockIdx.x * a.per_cta + warp * per_warp;
+  count_stretch(choice, lo, min(lo + per_warp, a.total), a.E, counters[warp], lane);
+  __syncthreads();
+  if (threadIdx.x < a.E) {
+    int sum = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) sum += counters[w][threadIdx.x];
+    a.counts[(int64_t)blockIdx.x * a.E + threadIdx.x] = sum;
+  }
+}
+
+template <bool ONE>
+__global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortArgs a) {
+  __shared__ int counters[kSortWarps][kMaxExperts];
+  __shared__ int before[4][kMaxExperts], all[4][kMaxExperts];            // of the pieces, in four parts
+  __shared__ int start[kMaxExperts], warp_sum[kMaxExperts / 32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, E = a.E;
+  for (int e = lane; e < E; e += 32) counters[warp][e] = 0;
+  __syncwarp();
+  chain_enter();
+  const int32_t* choice = after_enter(a.choice);
+  const int64_t per_warp = a.per_cta / kSortWarps, lo = blockIdx.x * a.per_cta + warp * per_warp, hi = min(lo + per_warp, a.total);
+  count_stretch(choice, lo, hi, E, counters[warp], lane);
+  const int e = threadIdx.x & (kMaxExperts - 1), part = threadIdx.x / kMaxExperts;
+  if constexpr (!ONE) {
+    const int* counts = after_enter((const int*)a.counts);
+    int b = 0, t = 0;
+    if (e < E)
+#pragma unroll 8
+      for (int p = part; p < a.pieces; p += 4) { const int c = __ldg(counts + (int64_t)p * E + e); t += c; if (p < (int)blockIdx.x) b += c; }
+    before[part][e] = b; all[part][e] = t;
+  }
+  __syncthreads();
+  // exclusive sums over the warps per expert, then over the experts
+  int total = 0;
+  if (part == 0) {
+    if (e < E) {
+      int run = 0;
+#pragma unroll
+      for (int w = 0; w < kSortWarps; ++w) { const int c = counters[w][e]; counters[w][e] = run; run += c; }
+      total = ONE ? run : all[0][e] + all[1][e] + all[2][e] + all[3][e];
+    }
+    int incl = total;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) { const int v = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += v; }
+    if (lane == 31) warp_sum[warp] = incl;
+    start[e] = incl - total;
+  }
+  __syncthreads();
+  if (part == 0) {
+    int first = start[e];
+    for (int w = 0; w < warp; ++w) first += warp_sum[w];
+    if (blockIdx.x == 0 && e < E) {
+      a.offsets[e] = first;
+      if (e == E - 1) a.offsets[E] = first + total;
+    }
+    start[e] = first + (ONE ? 0 : before[0][e] + before[1][e] + before[2][e] + before[3][e]);
+  }
+  __syncthreads();
+  int* mine = counters[warp];
+  for (int i = lane; i < E; i += 32) mine[i] += start[i];
+  __syncwarp();
+  constexpr int U = 8;
+  for (int64_t i = lo; i < hi; i += 32 * U) {
+    int x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) { const int64_t at = i + 32 * u + lane; x[u] = at < hi ? __ldg(choice + at) : -1; }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = i + 32 * u + lane;
+      const bool in = (unsigned)x[u] < (unsigned)E;
+      const unsigned peers = __match_any_sync(0xffffffffu, in ? x[u] : -1);
+      const int rank = __popc(peers & ((1u << lane) - 1));
+      const int row = in ? mine[x[u]] + rank : -1;
+      __syncwarp();
+      if (in && rank == 0) mine[x[u]] += __popc(peers);
+      __syncwarp();
+      if (at < hi) a.place[at] = row;
+      if (in) a.order[row] = (int)at;
+    }
+  }
+}
+
+// ---- rows ------------------------------------------------------------------------------------------------
+// A work item is a token's stretch of kPieces 16-byte pieces per lane, by a group of G lanes (8, 16 or 32: narrow rows share a
+// warp), so a few long rows occupy the card as well as many short ones.  Every piece of X is read once, by the token's item,
+// whatever the number of its rows.
+template <int G, int kPieces>
+__global__ void __launch_bounds__(256) dispatch_kernel(const uint4* X, const int32_t* place, uint4* X_s, int64_t items, int stretches, int pieces, int K,
+                                                       int64_t rows) {
+  chain_enter();
+  const uint4* x = after_enter(X);
+  const int32_t* pl = after_enter(place);
+  const int lane = threadIdx.x % G;
+  for (int64_t it = ((int64_t)blockIdx.x * 256 + threadIdx.x) / G; it < items; it += (int64_t)gridDim.x * 256 / G) {
+    const int64_t t = it / stretches;
+    const int p0 = (int)(it - t * stretches) * (G * kPieces) + lane;
+    uint4 v[kPieces];
+#pragma unroll
+    for (int u = 0; u < kPieces; ++u) if (p0 + u * G < pieces) v[u] = __ldg(x + t * pieces + p0 + u * G);
+#pragma unroll 4
+    for (int j = 0; j < K; ++j) {
+      const int r = __ldg(pl + t * K + j);
+      if ((unsigned)r >= (unsigned)rows) continue;
+      uint4* out = X_s + (int64_t)r * pieces;
+#pragma unroll
+      for (int u = 0; u < kPieces; ++u) if (p0 + u * G < pieces) out[p0 + u * G] = v[u];
+    }
+  }
+}
+
+// A 16-byte piece of Y is V values; the same V values of X_out or dX_out are 16 bytes, or 8 where Y is fp32 and they are bf16.
+template <typename T> struct Vec { static constexpr int V = 16 / sizeof(T); };
+template <typename T, int V> struct Pack;
+template <> struct Pack<float, 4> { using type = uint4; };
+template <> struct Pack<bf16, 8> { using type = uint4; };
+template <> struct Pack<bf16, 4> { using type = uint2; };
+
+__device__ __forceinline__ void unpack_word(unsigned w, float& a, float& b) { a = __uint_as_float(w << 16); b = __uint_as_float(w & 0xFFFF0000u); }
+template <typename T, int V> __device__ __forceinline__ void unpack(const typename Pack<T, V>::type& p, float* f) {
+  const unsigned* w = reinterpret_cast<const unsigned*>(&p);
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = __uint_as_float(w[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) unpack_word(w[i], f[2 * i], f[2 * i + 1]);
+  }
+}
+template <typename T, int V> __device__ __forceinline__ typename Pack<T, V>::type pack(const float* f) {
+  typename Pack<T, V>::type p;
+  unsigned* w = reinterpret_cast<unsigned*>(&p);
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) w[i] = __float_as_uint(f[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) { __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]); w[i] = *reinterpret_cast<unsigned*>(&h); }
+  }
+  return p;
+}
+
+// KB rows of a token are on their way at a time; the sum runs over j in ascending order, in fp32, and is rounded once.
+template <typename T, typename TY, int G, int kPieces>
+__global__ void __launch_bounds__(256) combine_rows_kernel(const uint4* Y, const float* weights, const int32_t* place, void* X_out, int64_t items,
+                                                           int stretches, int pieces, int K, int64_t rows) {
+  constexpr int V = Vec<TY>::V, KB = 4;
+  using Out = typename Pack<T, V>::type;
+  chain_enter();
+  const uint4* y = after_enter(Y);
+  const float* ws = after_enter(weights);
+  const int32_t* pl = after_enter(place);
+  const int lane = threadIdx.x % G;
+  for (int64_t it = ((int64_t)blockIdx.x * 256 + threadIdx.x) / G; it < items; it += (int64_t)gridDim.x * 256 / G) {
+    const int64_t t = it / stretches;
+    const int p0 = (int)(it - t * stretches) * (G * kPieces) + lane;
+    float acc[kPieces][V];
+#pragma unroll
+    for (int u = 0; u < kPieces; ++u)
+#pragma unroll
+      for (int i = 0; i < V; ++i) acc[u][i] = 0.f;
+    for (int j0 = 0; j0 < K; j0 += KB) {
+      int r[KB]; float w[KB]; uint4 v[KB][kPieces];
+#pragma unroll
+      for (int j = 0; j < KB; ++j) {
+        r[j] = j0 + j < K ? __ldg(pl + t * K + j0 + j) : -1;
+        w[j] = j0 + j < K && ws != nullptr ? __ldg(ws + t * K + j0 + j) : 1.f;
+      }
+#pragma unroll
+      for (int j = 0; j < KB; ++j)
+#pragma unroll
+        for (int u = 0; u < kPieces; ++u)
+          if ((unsigned)r[j] < (unsigned)rows && p0 + u * G < pieces) v[j][u] = __ldg(y + (int64_t)r[j] * pieces + p0 + u * G);
+#pragma unroll
+      for (int j = 0; j < KB; ++j) {
+        if ((unsigned)r[j] >= (unsigned)rows) continue;
+#pragma unroll
+        for (int u = 0; u < kPieces; ++u) {
+          float f[V];
+          unpack<TY, V>(v[j][u], f);
+#pragma unroll
+          for (int i = 0; i < V; ++i) acc[u][i] = fmaf(w[j], f[i], acc[u][i]);
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kPieces; ++u) if (p0 + u * G < pieces) ((Out*)X_out)[t * pieces + p0 + u * G] = pack<T, V>(acc[u]);
+  }
+}
+
+// A token is the work of WPT warps of a CTA: they share its pieces, so that dX_out is read once for KB of the token's rows, and the
+// dot products' parts are joined in a fixed order: lanes by halves, then the warps in turn.
+template <typename T, typename TY, int WPT>
+__global__ void __launch_bounds__(256) combine_backward_kernel(const void* dX_out, const uint4* Y, const float* weights, const int32_t* place, uint4* dY,
+                                                               float* dweights, int64_t n, int pieces, int K, int64_t rows) {
+  constexpr int V = Vec<TY>::V, KB = 4, kTokens = 8 / WPT;
+  using In = typename Pack<T, V>::type;
+  __shared__ float parts[8][KB];
+  chain_enter();
+  const In* g = after_enter((const In*)dX_out);
+  const uint4* y = after_enter(Y);
+  const float* ws = after_enter(weights);
+  const int32_t* pl = after_enter(place);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % WPT;
+  for (int64_t t0 = (int64_t)blockIdx.x * kTokens; t0 < n; t0 += (int64_t)gridDim.x * kTokens) {       // the same for the whole CTA
+    const int64_t t = t0 + warp / WPT;
+    const bool live = t < n;
+    for (int j0 = 0; j0 < K; j0 += KB) {
+      int r[KB]; float w[KB], dot[KB];
+#pragma unroll
+      for (int j = 0; j < KB; ++j) {
+        r[j] = live && j0 + j < K ? __ldg(pl + t * K + j0 + j) : -1;
+        w[j] = live && j0 + j < K ? __ldg(ws + t * K + j0 + j) : 0.f;
+        if ((unsigned)r[j] >= (unsigned)rows) r[j] = -1;
+        dot[j] = 0.f;
+      }
+      if (live) {
+#pragma unroll 2
+        for (int p = sub * 32 + lane; p < pieces; p += WPT * 32) {
+          const In gp = __ldg(g + t * pieces + p);
+          uint4 v[KB];
+#pragma unroll
+          for (int j = 0; j < KB; ++j) if (r[j] >= 0) v[j] = __ldg(y + (int64_t)r[j] * pieces + p);
+          float a[V];
+          unpack<T, V>(gp, a);
+#pragma unroll
+          for (int j = 0; j < KB; ++j) {
+            if (r[j] < 0) continue;
+            float f[V], o[V];
+            unpack<TY, V>(v[j], f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) { dot[j] = fmaf(a[i], f[i], dot[j]); o[i] = w[j] * a[i]; }
+            dY[(int64_t)r[j] * pieces + p] = pack<TY, V>(o);
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < KB; ++j)
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) dot[j] += __shfl_xor_sync(0xffffffffu, dot[j], o);
+      if constexpr (WPT == 1) {
+        if (live && lane < KB && j0 + lane < K) dweights[t * K + j0 + lane] = lane == 0 ? dot[0] : lane == 1 ? dot[1] : lane == 2 ? dot[2] : dot[3];
+      } else {
+        if (lane == 0)
+#pragma unroll
+          for (int j = 0; j < KB; ++j) parts[warp][j] = dot[j];
+        __syncthreads();
+        if (live && sub == 0 && lane < KB && j0 + lane < K) {
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < WPT; ++i) sum += parts[warp + i][lane];
+          dweights[t * K + j0 + lane] = sum;
+        }
+        __syncthreads();
+      }
+    }
+  }
+}
+
+int device_sms() {
+  int dev = 0, sms = 148;
+  cudaGetDevice(&dev);
+  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  return sms;
+}
+
+// Lanes per stretch: a warp for rows of 32 pieces and more
+int group_of(int pieces) { return pieces > 16 ? 32 : pieces > 8 ? 16 : 8; }
+unsigned item_grid(int64_t items, int group, int sms) {
+  const int64_t ctas = (items * group + 255) / 256, most = (int64_t)sms * 16;
+  return (unsigned)(ctas < most ? ctas : most);
+}
+
+template <int G>
+cudaError_t dispatch_with(const void* X, const int32_t* place, void* X_s, int64_t n, int pieces, int K, int sms, cudaStream_t st) {
+  constexpr int kPieces = 4;
+  const int stretches = (pieces + G * kPieces - 1) / (G * kPieces);
+  const int64_t items = n * stretches;
+  return launch_chained(dispatch_kernel<G, kPieces>, dim3(item_grid(items, G, sms)), dim3(256), 0, st, (const uint4*)X, place, (uint4*)X_s, items, stretches,
+                        pieces, K, n * K);
+}
+
+template <typename T, typename TY, int G>
+cudaError_t combine_with(const void* Y, const float* w, const int32_t* place, void* X_out, int64_t n, int pieces, int K, int sms, cudaStream_t st) {
+  constexpr int kPieces = 2;
+  const int stretches = (pieces + G * kPieces - 1) / (G * kPieces);
+  const int64_t items = n * stretches;
+  return launch_chained(combine_rows_kernel<T, TY, G, kPieces>, dim3(item_grid(items, G, sms)), dim3(256), 0, st, (const uint4*)Y, w, place, X_out, items,
+                        stretches, pieces, K, n * K);
+}
+template <typename T, typename TY>
+cudaError_t combine_of(const void* Y, const float* w, const int32_t* place, void* X_out, int64_t n, int d, int K, cudaStream_t st) {
+  const int pieces = d / Vec<TY>::V, sms = device_sms();
+  switch (group_of(pieces)) {
+    case 32: return combine_with<T, TY, 32>(Y, w, place, X_out, n, pieces, K, sms, st);
+    case 16: return combine_with<T, TY, 16>(Y, w, place, X_out, n, pieces, K, sms, st);
+    default: return combine_with<T, TY, 8>(Y, w, place, X_out, n, pieces, K, sms, st);
+  }
+}
+
+template <typename T, typename TY, int WPT>
+cudaError_t backward_with(const void* dX_out, const void* Y, const float* w, const int32_t* place, void* dY, float* dw, int64_t n, int pieces, int K,
+                          int sms, cudaStream_t st) {
+  const int64_t ctas = (n * WPT + 7) / 8, most = (int64_t)sms * 8;
+  return launch_chained(combine_backward_kernel<T, TY, WPT>, dim3((unsigned)(ctas < most ? ctas : most)), dim3(256), 0, st, dX_out, (const uint4*)Y, w, place,
+                        (uint4*)dY, dw, n, pieces, K, n * K);
+}
+template <typename T, typename TY>
+cudaError_t backward_of(const void* dX_out, const void* Y, const float* w, const int32_t* place, void* dY, float* dw, int64_t n, int d, int K, cudaStream_t st) {
+  const int pieces = d / Vec<TY>::V, sms = device_sms();
+  if (pieces <= 64) return backward_with<T, TY, 1>(dX_out, Y, w, place, dY, dw, n, pieces, K, sms, st);
+  if (pieces <= 128) return backward_with<T, TY, 2>(dX_out, Y, w, place, dY, dw, n, pieces, K, sms, st);
+  return backward_with<T, TY, 8>(dX_out, Y, w, place, dY, dw, n, pieces, K, sms, st);
+}
+
+}  // namespace
+
+size_t sort_scratch_bytes(int E) { return (size_t)kMaxPieces * E * 4; }
+
+cudaError_t launch_sort_tokens(const int32_t* choice, int64_t total, int E, int32_t* offsets, int32_t* order, int32_t* place, void* scratch, cudaStream_t st) {
+  SortArgs a{choice, offsets, order, place, (int*)scratch, total, 0, E, 1};
+  if (total <= kOnePiece) {
+    a.per_cta = (total + 1023) / 1024 * 1024;
+    return launch_chained(sort_place_kernel<true>, dim3(1), dim3(kSortThreads), 0, st, a);
+  }
+  a.per_cta = ((total + kMaxPieces - 1) / kMaxPieces + 1023) / 1024 * 1024;
+  a.pieces = (int)((total + a.per_cta - 1) / a.per_cta);
+  const cudaError_t e = launch_chained(sort_count_kernel, dim3(a.pieces), dim3(kSortThreads), 0, st, a);
+  return e != cudaSuccess ? e : launch_chained(sort_place_kernel<false>, dim3(a.pieces), dim3(kSortThreads), 0, st, a);
+}
+
+cudaError_t launch_dispatch(const void* X, const int32_t* place, void* X_s, int64_t n, int64_t row_bytes, int K, cudaStream_t st) {
+  const int pieces = (int)(row_bytes / 16), sms = device_sms();
+  switch (group_of(pieces)) {
+    case 32: return dispatch_with<32>(X, place, X_s, n, pieces, K, sms, st);
+    case 16: return dispatch_with<16>(X, place, X_s, n, pieces, K, sms, st);
+    default: return dispatch_with<8>(X, place, X_s, n, pieces, K, sms, st);
+  }
+}
+
+cudaError_t launch_combine_rows(int dtype, int y_dtype, const void* Y, const float* weights, const int32_t* place, void* X_out, int64_t n, int d, int K,
+                                cudaStream_t st) {
+  if (dtype == 0) return combine_of<float, float>(Y, weights, place, X_out, n, d, K, st);
+  return y_dtype == 0 ? combine_of<bf16, float>(Y, weights, place, X_out, n, d, K, st) : combine_of<bf16, bf16>(Y, weights, place, X_out, n, d, K, st);
+}
+
+cudaError_t launch_combine_backward(int dtype, int y_dtype, const void* dX_out, const void* Y, const float* weights, const int32_t* place, void* dY,
+                                    float* dweights, int64_t n, int d, int K, cudaStream_t st) {
+  if (dtype == 0) return backward_of<float, float>(dX_out, Y, weights, place, dY, dweights, n, d, K, st);
+  return y_dtype == 0 ? backward_of<bf16, float>(dX_out, Y, weights, place, dY, dweights, n, d, K, st)
+                      : backward_of<bf16, bf16>(dX_out, Y, weights, place, dY, dweights, n, d, K, st);
+}
+
+}  // namespace ecmoe
