@@ -333,6 +333,60 @@ ec_status ec_combine(const ec_sort_config* cfg, const void* Y, const float* weig
 ec_status ec_combine_backward(const ec_sort_config* cfg, const void* dX_out, const void* Y, const float* weights,
                               const int32_t* place, void* dY, float* dweights, void* cuda_stream);
 
+/*
+ * Expert products on 4-bit operands (the paper has no counterpart): the OCP microscaled format with e2m1 elements, for serving
+ * a layer whose weights are what a forward pass reads.  Blocks of 32 values along the contraction share a power of two 2^(s - 127),
+ * s = max(0, floor(log2 amax) + 125); a value is +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} times it, to the nearest (ties to the even code) and 6
+ * where it is beyond.  A block that holds an infinity or a NaN has s = 255 and stands for NaN throughout.
+ * A matrix of `cols` columns (the contraction) is two arrays, both dense and 16-byte aligned:
+ *   codes  [rows, ec_mx_code_pitch(cols)]   16 bytes per block, value 2 i of a row in the low four bits of byte i; a last block that
+ *                                           cols does not fill holds zeros (code 0) behind it
+ *   scales [rows, ec_mx_scale_pitch(cols)]  a byte s per block; bytes behind the last block's are padding (written as 0 by the
+ *                                           quantisation, never read by the product)
+ * Matrices of several experts or batches follow one another.  Restrictions (EC_ERR_UNSUPPORTED): rows of a matrix in fp32 or bf16
+ * a multiple of 16 bytes long; rows and columns <= 2^22 - 64 (rows of A: < 2^31 - 256); batches * rows < 2^31.
+ */
+int64_t ec_mx_code_pitch(int64_t cols);   /* 16 * ceil(cols / 32); 0 if cols < 1 */
+int64_t ec_mx_scale_pitch(int64_t cols);  /* 16 * ceil(cols / 512); 0 if cols < 1 */
+
+/* X [batches, rows, cols] of `dtype` into the format, or with transposed = 1 X [batches, cols, rows]: the contraction runs along the
+ * rows of what is stored (W1 [E, d, d'] becomes [E, d'] rows of d), rows is then what must fill 16-byte rows.  batches = 0 or rows = 0:
+ * nothing to do. */
+ec_status ec_mx_quantize(int dtype, const void* X, int64_t batches, int64_t rows, int64_t cols, int transposed, uint8_t* codes,
+                         uint8_t* scales, void* cuda_stream);
+
+/* The values that codes and scales stand for, X [rows, cols] of `dtype` (exact in either type, but for what exceeds its range). */
+ec_status ec_mx_dequantize(int dtype, const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, void* X,
+                           void* cuda_stream);
+
+/* ec_dispatch with 4-bit rows: the quantised row of X (cfg->dtype) of token t goes to the rows place[t, j] of codes and scales
+ * [n * per_token, ...]; the others are left as they were. */
+ec_status ec_mx_dispatch(const ec_sort_config* cfg, const void* X, const int32_t* place, uint8_t* codes, uint8_t* scales,
+                         void* cuda_stream);
+
+typedef enum { EC_MX_NONE = 0, EC_MX_GELU_ERF = 1, EC_MX_GELU_TANH = 2 } ec_mx_act;
+typedef enum { EC_MX_OUT_F32 = 0, EC_MX_OUT_BF16 = 1, EC_MX_OUT_MX = 2 } ec_mx_out;
+typedef struct {
+  int64_t rows;       /* rows of A and C                                       */
+  int32_t N, K, E;    /* columns of C, the contraction, experts (1 <= E <= 256) */
+  int32_t out;        /* ec_mx_out: the type of C                              */
+  int32_t act;        /* ec_mx_act, applied to the product with its bias       */
+  int32_t bias_dtype; /* ec_dtype of bias                                      */
+} ec_mx_gemm_config;
+
+/*
+ * C[r, :] = act(A[r, :] . B[e]^T + bias[e, :]) for the rows offsets[e] <= r < offsets[e + 1] of expert e: groups of any length,
+ * also none.  A [rows, K] and B [E, N, K] in the format above, offsets [E + 1] as ec_sort_tokens writes them (or i * k for the slots
+ * of expert choice), bias [E, N] or NULL; C [rows, N] fp32 or bf16, dense, or the codes of the result as blocks along N with its scales
+ * in C_scales (NULL otherwise), ready to be the next product's A.  Products are exact, sums fp32, bias and act fp32, one rounding.  Rows
+ * of no expert are left as they were.  offsets that decrease or leave [0, rows] are read as if cut to that range: every access
+ * stays inside the arrays.  rows = 0: nothing to do.  `ws`: 256 bytes, 256-byte aligned, for the status word (ec_read_status).
+ */
+#define EC_MX_WORKSPACE_BYTES 256
+ec_status ec_mx_expert_gemm(const ec_mx_gemm_config* cfg, const uint8_t* A, const uint8_t* A_scales, const int32_t* offsets,
+                            const uint8_t* B, const uint8_t* B_scales, const void* bias, void* C, uint8_t* C_scales, void* ws,
+                            size_t ws_bytes, void* cuda_stream);
+
 /* 1 if this library was built with -DEC_DEBUG: every kernel then range-checks each index it reads from I, row_ptr
  * or slots before using it, skips the access when it is out of range and records EC_ERR_INDEX in the status word
  * (ec_read_status).  The normal build compiles these checks out. */

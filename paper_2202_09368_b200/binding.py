@@ -27,9 +27,13 @@ EXPORTS = ["ec_capacity", "ec_workspace_bytes", "ec_saved_bytes", "ec_saved_view
            "ec_uses_tensor_cores", "ec_launch_count", "ec_profile_enable", "ec_profile_read",
            "ec_route_static", "ec_route_static_bytes", "ec_shuffle", "ec_unshuffle",
            "ec_forward_only_workspace_bytes", "ec_capped_assignment", "ec_route_token_choice", "ec_expert_gemm", "ec_validate_routing", "ec_debug_build", "ec_backward_view",
-           "ec_sort_workspace_bytes", "ec_sort_tokens", "ec_dispatch", "ec_combine", "ec_combine_backward"]
+           "ec_sort_workspace_bytes", "ec_sort_tokens", "ec_dispatch", "ec_combine", "ec_combine_backward",
+           "ec_mx_code_pitch", "ec_mx_scale_pitch", "ec_mx_quantize", "ec_mx_dequantize", "ec_mx_dispatch", "ec_mx_expert_gemm"]
 EC_GEMM_XW1, EC_GEMM_HW2T, EC_GEMM_ATB = 0, 1, 2
+EC_MX_NONE, EC_MX_GELU_ERF, EC_MX_GELU_TANH = 0, 1, 2
+EC_MX_OUT_F32, EC_MX_OUT_BF16, EC_MX_OUT_MX = 0, 1, 2
 EC_ROUTE_STATIC_SCRATCH_BYTES = 8 << 20
+EC_MX_WORKSPACE_BYTES = 256
 
 
 class ec_config(C.Structure):
@@ -51,6 +55,10 @@ class ec_backward_ptrs(C.Structure):
 class ec_sort_config(C.Structure):
     _fields_ = [("n", C.c_int64), ("d_model", C.c_int32), ("E", C.c_int32), ("per_token", C.c_int32), ("dtype", C.c_int32),
                 ("y_dtype", C.c_int32)]
+
+
+class ec_mx_gemm_config(C.Structure):
+    _fields_ = [("rows", C.c_int64)] + [(name, C.c_int32) for name in ("N", "K", "E", "out", "act", "bias_dtype")]
 
 
 class EcError(RuntimeError):
@@ -106,6 +114,14 @@ def lib():
         L.ec_dispatch.restype = C.c_int; L.ec_dispatch.argtypes = [Q, V, V, V, V]
         L.ec_combine.restype = C.c_int; L.ec_combine.argtypes = [Q, V, V, V, V, V]
         L.ec_combine_backward.restype = C.c_int; L.ec_combine_backward.argtypes = [Q, V, V, V, V, V, V, V]
+        I64 = C.c_int64
+        L.ec_mx_code_pitch.restype = I64; L.ec_mx_code_pitch.argtypes = [I64]
+        L.ec_mx_scale_pitch.restype = I64; L.ec_mx_scale_pitch.argtypes = [I64]
+        L.ec_mx_quantize.restype = C.c_int; L.ec_mx_quantize.argtypes = [C.c_int, V, I64, I64, I64, C.c_int, V, V, V]
+        L.ec_mx_dequantize.restype = C.c_int; L.ec_mx_dequantize.argtypes = [C.c_int, V, V, I64, I64, V, V]
+        L.ec_mx_dispatch.restype = C.c_int; L.ec_mx_dispatch.argtypes = [Q, V, V, V, V, V]
+        L.ec_mx_expert_gemm.restype = C.c_int
+        L.ec_mx_expert_gemm.argtypes = [C.POINTER(ec_mx_gemm_config), V, V, V, V, V, V, V, V, V, C.c_size_t, V]
         _lib = L
     return _lib
 
@@ -353,6 +369,113 @@ def ec_combine_backward(cfg, dX_out, Y, weights, place, dY=None, dweights=None):
                                 (place, torch.int32, (n, K)), (dY, ty, (n * K, d)), (dweights, torch.float32, (n, K)))
     _check(lib().ec_combine_backward(C.byref(cfg), g, y, w, p, dy, dw, stream), "ec_combine_backward")
     return dY, dweights
+
+
+# ---- products on 4-bit operands ------------------------------------------------------------------------------------------------
+
+@dataclass
+class Mx:
+    """A matrix (or several: leading axes) in the 4-bit microscaled format."""
+    codes: torch.Tensor        # [..., rows, code pitch] uint8
+    scales: torch.Tensor       # [..., rows, scale pitch] uint8
+    cols: int                  # columns: the contraction
+
+
+def _mx_pitches(cols):
+    return 16 * -(-cols // 32), 16 * -(-cols // 512)
+
+
+def alloc_mx(shape, device="cuda") -> Mx:
+    """Memory for a matrix [..., rows, cols] in the format."""
+    codes, scales = _mx_pitches(shape[-1])
+    return Mx(torch.empty(*shape[:-1], codes, dtype=torch.uint8, device=device), torch.empty(*shape[:-1], scales, dtype=torch.uint8, device=device), shape[-1])
+
+
+def _mx_operands(what, dev, q, shape):
+    """Addresses of a matrix in the format whose values have this shape."""
+    codes, scales = _mx_pitches(shape[-1])
+    if q.cols != shape[-1]:
+        raise EcError(EC_ERR_INVALID_ARG, f"{what}: wanted {shape[-1]} columns, got {q.cols}")
+    return _dense(what, dev, (q.codes, torch.uint8, shape[:-1] + (codes,)), (q.scales, torch.uint8, shape[:-1] + (scales,)))
+
+
+def _dtype_code(what, dtype):
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise EcError(EC_ERR_INVALID_ARG, f"{what}: wanted float32 or bfloat16, got {dtype}")
+    return EC_F32 if dtype is torch.float32 else EC_BF16
+
+
+def ec_mx_quantize(X, transposed=False, out: Mx | None = None) -> Mx:
+    """X [..., rows, cols], or with `transposed` [..., cols, rows], in the 4-bit format with blocks along cols."""
+    dev, dt = X.device, _dtype_code("ec_mx_quantize", X.dtype)
+    stream = _stream_of("ec_mx_quantize", dev)
+    if X.dim() < 2:
+        raise EcError(EC_ERR_INVALID_ARG, "ec_mx_quantize: wanted a matrix")
+    lead, (rows, cols) = tuple(X.shape[:-2]), (X.shape[:-3:-1] if transposed else X.shape[-2:])
+    batches = 1
+    for v in lead:
+        batches *= v
+    if cols < 1:
+        raise EcError(EC_ERR_INVALID_ARG, "ec_mx_quantize: no columns")
+    out = alloc_mx(lead + (rows, cols), dev) if out is None else out
+    x, = _dense("ec_mx_quantize", dev, (X, X.dtype, X.shape))
+    q, s = _mx_operands("ec_mx_quantize", dev, out, lead + (rows, cols))
+    _check(lib().ec_mx_quantize(dt, x, batches, rows, cols, int(bool(transposed)), q, s, stream), "ec_mx_quantize")
+    return out
+
+
+def ec_mx_dequantize(q: Mx, dtype=torch.bfloat16, out=None):
+    """The values that q stands for, [..., rows, cols] of `dtype` (out's, when it is given)."""
+    dev, shape = q.codes.device, tuple(q.codes.shape[:-1]) + (q.cols,)
+    stream = _stream_of("ec_mx_dequantize", dev)
+    out = torch.empty(shape, dtype=dtype, device=dev) if out is None else out
+    dt = _dtype_code("ec_mx_dequantize", out.dtype)
+    c, s = _mx_operands("ec_mx_dequantize", dev, q, shape)
+    x, = _dense("ec_mx_dequantize", dev, (out, out.dtype, shape))
+    rows = 1
+    for v in shape[:-1]:
+        rows *= v
+    _check(lib().ec_mx_dequantize(dt, c, s, rows, q.cols, x, stream), "ec_mx_dequantize")
+    return out
+
+
+def ec_mx_dispatch(cfg, X, place, out: Mx | None = None) -> Mx:
+    """ec_dispatch with rows in the 4-bit format: [n * per_token, d_model]; rows that no choice holds are left as they were."""
+    dev, n, K, d = X.device, cfg.n, cfg.per_token, cfg.d_model
+    stream = _stream_of("ec_mx_dispatch", dev)
+    out = alloc_mx((n * K, d), dev) if out is None else out
+    x, p = _dense("ec_mx_dispatch", dev, (X, _TYPES[cfg.dtype], (n, d)), (place, torch.int32, (n, K)))
+    q, s = _mx_operands("ec_mx_dispatch", dev, out, (n * K, d))
+    _check(lib().ec_mx_dispatch(C.byref(cfg), x, p, q, s, stream), "ec_mx_dispatch")
+    return out
+
+
+_ACTS = {"none": EC_MX_NONE, "erf": EC_MX_GELU_ERF, "tanh": EC_MX_GELU_TANH}
+
+
+def ec_mx_expert_gemm(A: Mx, W: Mx, offsets, bias=None, act="none", out=None, dtype=torch.bfloat16, ws=None):
+    """act(A[r] . W[e]^T + bias[e]) for the rows offsets[e] <= r < offsets[e + 1]: A [rows, K], W [E, N, K].  out: a tensor [rows, N] (None:
+    a new one of `dtype`) or an Mx to receive the result in the 4-bit format.  act: "none", "erf" or "tanh" (GeLU).  Rows of no
+    expert are left as they were."""
+    what, dev, (rows, _), (E, N, _), K = "ec_mx_expert_gemm", A.codes.device, A.codes.shape, W.codes.shape, W.cols
+    stream = _stream_of(what, dev)
+    out = torch.empty(rows, N, dtype=dtype, device=dev) if out is None else out
+    ws = torch.empty(EC_MX_WORKSPACE_BYTES, dtype=torch.uint8, device=dev) if ws is None else ws
+    a, sa = _mx_operands(what, dev, A, (rows, K))
+    b, sb = _mx_operands(what, dev, W, (E, N, K))
+    o, w = _dense(what, dev, (offsets, torch.int32, (E + 1,)), (ws, torch.uint8, ws.shape))
+    if isinstance(out, Mx):
+        (c, sc), kind = _mx_operands(what, dev, out, (rows, N)), EC_MX_OUT_MX
+    else:
+        kind, sc = (EC_MX_OUT_F32 if _dtype_code(what, out.dtype) == EC_F32 else EC_MX_OUT_BF16), None
+        c, = _dense(what, dev, (out, out.dtype, (rows, N)))
+    bp, bt = None, EC_F32
+    if bias is not None:
+        bt = _dtype_code(what, bias.dtype)
+        bp, = _dense(what, dev, (bias, bias.dtype, (E, N)))
+    cfg = ec_mx_gemm_config(rows, N, K, E, kind, _ACTS[act], bt)
+    _check(lib().ec_mx_expert_gemm(C.byref(cfg), a, sa, o, b, sb, bp, c, sc, w, ws.numel(), stream), what)
+    return out
 
 
 def ec_validate_routing(cfg, I, row_ptr, slots, ws=None) -> int:

@@ -1,4 +1,4 @@
-// C ABI of the tokens sorted by expert: argument checks and launches.
+// C ABI of the tokens sorted by expert and of the products on 4-bit operands: argument checks and launches.
 #include "../../include/ecmoe.h"
 #include "internal.h"
 
@@ -60,5 +60,59 @@ ec_status ec_combine_backward(const ec_sort_config* c, const void* dX_out, const
   if (s != EC_OK || c->n == 0) return s;
   if (bad_pointers(dX_out, Y, weights, place, dY, dweights)) return EC_ERR_INVALID_ARG;
   EC_CUDA(launch_combine_backward(c->dtype, c->y_dtype, dX_out, Y, weights, place, dY, dweights, c->n, c->d_model, c->per_token, (cudaStream_t)stream));
+  return EC_OK;
+}
+
+// ---- 4-bit operands --------------------------------------------------------------------------------------------
+namespace {
+constexpr int64_t kMxMost = (1 << 22) - 64;
+}
+
+int64_t ec_mx_code_pitch(int64_t cols) { return cols < 1 ? 0 : 16 * ((cols - 1) / 32 + 1); }
+int64_t ec_mx_scale_pitch(int64_t cols) { return cols < 1 ? 0 : 16 * ((cols - 1) / 512 + 1); }
+
+ec_status ec_mx_quantize(int dtype, const void* X, int64_t batches, int64_t rows, int64_t cols, int transposed, uint8_t* codes, uint8_t* scales, void* stream) {
+  if ((dtype != EC_F32 && dtype != EC_BF16) || (transposed != 0 && transposed != 1) || batches < 0 || rows < 0 || cols < 1) return EC_ERR_INVALID_ARG;
+  // a transposed matrix has its rows on the grid and a 32-bit index inside one; rows as they are only add up
+  if (cols > kMxMost || (transposed && rows > kMxMost) || batches >= ((int64_t)1 << 31) || rows >= ((int64_t)1 << 31)) return EC_ERR_UNSUPPORTED;
+  if (batches * rows >= ((int64_t)1 << 31) || ((transposed ? rows : cols) * esize(dtype)) % 16) return EC_ERR_UNSUPPORTED;
+  if (batches == 0 || rows == 0) return EC_OK;
+  if (bad_pointers(X, codes, scales)) return EC_ERR_INVALID_ARG;
+  EC_CUDA(launch_mx_quantize(dtype, X, batches, (int)rows, (int)cols, transposed, codes, scales, (cudaStream_t)stream));
+  return EC_OK;
+}
+
+ec_status ec_mx_dequantize(int dtype, const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, void* X, void* stream) {
+  if ((dtype != EC_F32 && dtype != EC_BF16) || rows < 0 || cols < 1) return EC_ERR_INVALID_ARG;
+  if (cols > kMxMost || rows >= ((int64_t)1 << 31) || (cols * esize(dtype)) % 16) return EC_ERR_UNSUPPORTED;
+  if (rows == 0) return EC_OK;
+  if (bad_pointers(codes, scales, X)) return EC_ERR_INVALID_ARG;
+  EC_CUDA(launch_mx_dequantize(dtype, codes, scales, rows, (int)cols, X, (cudaStream_t)stream));
+  return EC_OK;
+}
+
+ec_status ec_mx_dispatch(const ec_sort_config* c, const void* X, const int32_t* place, uint8_t* codes, uint8_t* scales, void* stream) {
+  const ec_status s = check_sort(c);
+  if (s != EC_OK || c->n == 0) return s;
+  if (bad_pointers(X, place, codes, scales)) return EC_ERR_INVALID_ARG;
+  EC_CUDA(launch_mx_dispatch(c->dtype, X, place, c->n, c->d_model, c->per_token, codes, scales, (cudaStream_t)stream));
+  return EC_OK;
+}
+
+ec_status ec_mx_expert_gemm(const ec_mx_gemm_config* c, const uint8_t* A, const uint8_t* A_scales, const int32_t* offsets, const uint8_t* B,
+                            const uint8_t* B_scales, const void* bias, void* C, uint8_t* C_scales, void* ws, size_t ws_bytes, void* stream) {
+  if (!c || c->rows < 0 || c->N < 1 || c->K < 1 || c->E < 1) return EC_ERR_INVALID_ARG;
+  if (c->out < EC_MX_OUT_F32 || c->out > EC_MX_OUT_MX || c->act < EC_MX_NONE || c->act > EC_MX_GELU_TANH) return EC_ERR_INVALID_ARG;
+  if (c->bias_dtype != EC_F32 && c->bias_dtype != EC_BF16) return EC_ERR_INVALID_ARG;
+  if (c->E > 256 || c->N > kMxMost || c->K > kMxMost || c->rows >= ((int64_t)1 << 31) - 256) return EC_ERR_UNSUPPORTED;
+  if ((c->out == EC_MX_OUT_F32 && c->N % 4) || (c->out == EC_MX_OUT_BF16 && c->N % 8)) return EC_ERR_UNSUPPORTED;
+  if ((c->rows / 32 + c->E + 1) * ((c->N + 127) / 128) >= ((int64_t)1 << 31)) return EC_ERR_UNSUPPORTED;      // tiles are counted in 32 bits
+  if (ws == nullptr || misaligned(ws, 256)) return EC_ERR_INVALID_ARG;
+  if (ws_bytes < EC_MX_WORKSPACE_BYTES) return EC_ERR_WORKSPACE;
+  if (c->rows == 0) return EC_OK;
+  if (bad_pointers(A, A_scales, offsets, B, B_scales, C) || (bias != nullptr && misaligned(bias, 16))) return EC_ERR_INVALID_ARG;
+  if (c->out == EC_MX_OUT_MX ? bad_pointers(C_scales) : C_scales != nullptr) return EC_ERR_INVALID_ARG;
+  MxGemmArgs g{c->rows, c->N, c->K, c->E, c->out, c->act, A, A_scales, offsets, B, B_scales, bias, c->bias_dtype, C, C_scales, (int*)ws};
+  EC_CUDA(launch_gemm_mx(g, (cudaStream_t)stream));
   return EC_OK;
 }

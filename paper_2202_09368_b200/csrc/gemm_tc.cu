@@ -949,6 +949,9 @@ cudaError_t launch_bn(int bn, int ctas, const CUtensorMap& ta, const CUtensorMap
 
 }  // namespace
 
+void* tensor_map_encoder() { return (void*)get_encode(); }
+cudaError_t bind_device_context(int dev) { return bind_context(dev); }
+
 bool tc_gemm_supported(const TcGemmArgs& g) {
   if (g.M < 1 || g.N < 1 || g.K < 1 || g.batches < 1) return false;
   if (g.lda % 8 || g.ldb % 8 || g.ldc % 8 || g.N % 8) return false;            // 16-byte rows and vector stores

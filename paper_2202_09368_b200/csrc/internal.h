@@ -184,6 +184,19 @@ cudaError_t launch_combine_rows(int dtype, int y_dtype, const void* Y, const flo
 cudaError_t launch_combine_backward(int dtype, int y_dtype, const void* dX_out, const void* Y, const float* weights,
                                     const int32_t* place, void* dY, float* dweights, int64_t n, int d, int K, cudaStream_t st);
 
+// ---- 4-bit microscaled format (mx.cu, gemm_mx.cu) ------------------------------------------------
+cudaError_t launch_mx_quantize(int dtype, const void* X, int64_t batches, int rows, int cols, int transposed, uint8_t* codes, uint8_t* scales, cudaStream_t st);
+cudaError_t launch_mx_dequantize(int dtype, const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols, void* X, cudaStream_t st);
+cudaError_t launch_mx_dispatch(int dtype, const void* X, const int32_t* place, int64_t n, int d, int K, uint8_t* codes, uint8_t* scales, cudaStream_t st);
+struct MxGemmArgs {
+  int64_t rows; int N, K, E;
+  int out, act;                                    // EC_MX_OUT_*, EC_MX_*
+  const void* A; const uint8_t* A_scales; const int32_t* offsets; const void* B; const uint8_t* B_scales;
+  const void* bias; int bias_dtype;                // [E, N] or null
+  void* C; uint8_t* C_scales; int* status;
+};
+cudaError_t launch_gemm_mx(const MxGemmArgs& g, cudaStream_t st);
+
 // ---- plain FMA GEMM (gemm_simt.cu) -------------------------------------------------------------
 enum Epilogue { EPI_STORE = 0, EPI_GELU = 1, EPI_GELU_GRAD = 2, EPI_ADD_SLOTS = 3 };
 
@@ -275,6 +288,8 @@ struct TcGemmArgs {
   int silent;        // debug build: the first CTA loads nothing, see ec_debug_gate_wait
 };
 constexpr int EPI_SOFTMAX = 4;
+void* tensor_map_encoder();                  // the driver's cuTensorMapEncodeTiled (PFN_cuTensorMapEncodeTiled_v12000), or null
+cudaError_t bind_device_context(int dev);    // the encoder wants a context: makes the device's current where the thread has none
 bool tc_gemm_supported(const TcGemmArgs& g);
 cudaError_t launch_gemm_tc(const TcGemmArgs& g, cudaStream_t st);
 
