@@ -7,13 +7,16 @@
 // of C, a column of it a row.
 //
 // Per CTA (persistent, one per SM):
-//   warp 0      TMA: stages of 256 of the contraction, 128 x 128 bytes of B and NT x 128 bytes of A
-//   warp 1      one lane issues the MMAs, 64 of the contraction each
-//   warps 2-5   epilogue, a quarter of tensor memory's lanes each
-//   warps 6-9   scales: 512 of the contraction (16 bytes of a row's scales) at a time, from global memory through registers into
-//               tensor memory, where every quarter of the lanes wants its own copy: row 32 c + l of a tile in lane l, column c, four
-//               blocks' bytes to a column.  Rows start anywhere, so no prepared layout could serve them.
-// Two accumulators of NT columns, two buffers of scales of 16 + 4 * cols_a columns.
+//   warp 0       TMA: stages of 256 of the contraction, 128 x 128 bytes of B and NT x 128 bytes of A, and their scales, 1024 of the
+//                contraction (32 bytes of a row's scales) at a time
+//   warp 1       the MMAs, 64 of the contraction each
+//   warps 2-9    epilogue, two for each quarter of tensor memory's lanes
+//   warps 10-13  scales: a stage's from shared through registers into tensor memory, where every quarter of the lanes wants its own
+//                copy: row 32 c + l of a tile in lane l, column c, four blocks' bytes to a column.  Rows start anywhere, so no
+//                prepared layout could serve them.
+// Two accumulators of NT columns, and as many buffers of scales as there are stages: a stage is full when its operands have landed and
+// its scales are in tensor memory, and one commit frees both.  (A wait that is over at once still takes the MMA warp 100 cycles, a commit
+// 60 to 100, issuing an MMA 80: with barriers of their own for the scales a stage took 815 cycles beside the MMAs' 384.)
 #include "../../include/ecmoe.h"
 #include "internal.h"
 #include "mx.cuh"
@@ -29,23 +32,28 @@ namespace {
 constexpr int kM = 128;                              // columns of C per tile
 constexpr int kStageK = 256, kRowBytes = kStageK / 2;
 constexpr int kBBytes = kM * kRowBytes;              // 16 KiB
-constexpr int kEpi = 4, kScaleWarps = 4;
+constexpr int kEpi = 8, kScaleWarps = 4;
 constexpr int kThreads = 32 * (2 + kEpi + kScaleWarps);
 constexpr int kMaxE = 256;
 constexpr int kTmemCols = 512;
-constexpr int kSmemBudget = 220 * 1024;
+constexpr int kScaleStages = 2, kScaleStageK = 1024, kScaleRow = kScaleStageK / 32;
+constexpr int kSmemBudget = 221 * 1024;
 
-__host__ __device__ constexpr int stages_of(int nt) { const int fit = kSmemBudget / (kBBytes + nt * kRowBytes); return fit > 10 ? 10 : fit; }
-// Columns of tensor memory for 128 of the contraction of A's scales.  tcgen05.mma wants a scale matrix to begin at a multiple of four
-// columns, so narrow tiles leave some of the four unused.
+__host__ __device__ constexpr int scale_stage_bytes(int nt) { return (kM + nt) * kScaleRow; }
+__host__ __device__ constexpr int stages_of(int nt) {
+  const int fit = (kSmemBudget - kScaleStages * scale_stage_bytes(nt)) / (kBBytes + nt * kRowBytes);
+  return fit > 10 ? 10 : fit;
+}
+// Columns of tensor memory for 128 of the contraction of A's scales, and for a stage's of both.  tcgen05.mma wants a scale matrix to begin
+// at a multiple of four columns, so narrow tiles leave some of the four unused.
 __host__ __device__ constexpr int cols_a(int nt) { return nt <= 128 ? 4 : 8; }
+__host__ __device__ constexpr int scale_cols(int nt) { return 8 + 2 * cols_a(nt); }
 
 struct MxParams {
   int64_t rows;
   int N, E, tiles_m, blocks, kblocks;                // blocks: of 32 along the contraction; kblocks: stages of 256
   int act;
   const int32_t* offsets;
-  const uint8_t* a_scales; const uint8_t* b_scales; int64_t scale_pitch;
   const void* bias; int bias_f32;
   void* c; uint8_t* c_scales; int64_t c_pitch, c_scale_pitch;     // c_pitch in bytes
   int* status;
@@ -53,28 +61,55 @@ struct MxParams {
 
 enum { OUT_F32 = 0, OUT_BF16 = 1, OUT_MX = 2 };
 
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1) {
-  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-               ::"r"(dst), "l"(tm), "r"(bar), "r"(c0), "r"(c1) : "memory");
+// The TMA and the MMA warp run as whole warps with the same values in every lane, and one lane, chosen once, carries out what must be done
+// once: the compiler then keeps descriptors, addresses and loop counters in uniform registers, where these instructions want them.
+// (Inside `if (lane == 0)` every operand is moved there before each instruction: 430 cycles to issue four MMAs of 96.)
+__device__ __forceinline__ uint32_t elect_one() {
+  uint32_t r;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(r));
+  return r;
 }
-__device__ __forceinline__ void tc_mma_mx(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
-  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
-               " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
-               ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory");
+// Clears `alive` when the wait runs out or another role has given up; what the caller then does up to its loop's end it does with its
+// lead taken away.
+__device__ __forceinline__ void wait(uint32_t& alive, uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int where) {
+  if (alive && !mbar_try(bar, parity)) alive = mbar_wait(bar, parity, abort_flag, status, where);
 }
-__device__ __forceinline__ void tc_st4(uint32_t taddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+__device__ __forceinline__ void expect_tx_if(uint32_t lead, uint32_t bar, uint32_t bytes) {
+  asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %2, 0;\n @q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n}\n" ::"r"(bar), "r"(bytes), "r"(lead) : "memory");
 }
-__device__ __forceinline__ void tc_st2(uint32_t taddr, uint32_t a, uint32_t b) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};" ::"r"(taddr), "r"(a), "r"(b) : "memory");
+__device__ __forceinline__ void tma_load_2d_if(uint32_t lead, uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1) {
+  asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %5, 0;\n"
+               " @q cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];\n}\n"
+               ::"r"(dst), "l"(tm), "r"(bar), "r"(c0), "r"(c1), "r"(lead) : "memory");
 }
-__device__ __forceinline__ void tc_st1(uint32_t taddr, uint32_t a) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "r"(a) : "memory");
+__device__ __forceinline__ void tma_load_3d_if(uint32_t lead, uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1, int c2) {
+  asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %6, 0;\n"
+               " @q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];\n}\n"
+               ::"r"(dst), "l"(tm), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(lead) : "memory");
+}
+__device__ __forceinline__ void tc_commit_if(uint32_t lead, uint32_t bar) {
+  asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n"
+               ::"r"(bar), "r"(lead) : "memory");
+}
+// Descriptors by their lower words (address and leading offset); the upper one is that of make_desc(., 16, 1024).
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_low(uint32_t saddr) { return ((saddr & 0x3FFFFu) >> 4) | (1u << 16); }
+__device__ __forceinline__ void tc_mma_mx_if(uint32_t lead, uint32_t d, uint32_t alow, uint32_t blow, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+  asm volatile("{\n .reg .pred p, q;\n .reg .b64 a, b;\n mov.b64 a, {%1, %8};\n mov.b64 b, {%2, %8};\n setp.ne.b32 p, %6, 0;\n setp.ne.b32 q, %7, 0;\n"
+               " @q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, %3, [%4], [%5], p;\n}\n"
+               ::"r"(d), "r"(alow), "r"(blow), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate), "r"(lead), "n"(kDescHigh) : "memory");
+}
+// A warp's wait with an answer: one lane polls.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int where, int lane) {
+  bool ok = true;
+  if (lane == 0) ok = mbar_wait(bar, parity, abort_flag, status, where);
+  return __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+}
+__device__ __forceinline__ void tc_st8(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
 __device__ __forceinline__ void tc_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-// word g of a row's 16 scale bytes
-__device__ __forceinline__ unsigned word(const uint4& v, int g) { return g == 0 ? v.x : g == 1 ? v.y : g == 2 ? v.z : v.w; }
 
 // Where a tile lies.  Tiles run expert by expert, inside one along its row tiles first: those that run at the same time share weights.
 struct Tile { int e, m, row0, rows; };
@@ -91,30 +126,31 @@ __device__ __forceinline__ Tile find_tile(const Groups* g, int tiles_m, int tile
 
 template <int NT, int OUT>
 __global__ void __launch_bounds__(kThreads, 1)
-gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const MxParams p) {
-  constexpr int S = stages_of(NT), kStage = kBBytes + NT * kRowBytes;
-  constexpr int kColsA = cols_a(NT), kScaleCols = 16 + 4 * kColsA, kScales0 = 2 * NT;
-  static_assert(kScales0 + 2 * kScaleCols <= kTmemCols, "tensor memory");
+gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmAs,
+               const __grid_constant__ CUtensorMap tmBs, const MxParams p) {
+  constexpr int S = stages_of(NT), kStage = kBBytes + NT * kRowBytes, kScaleStage = scale_stage_bytes(NT);
+  constexpr int kColsA = cols_a(NT), kScaleCols = scale_cols(NT), kScales0 = 2 * NT;
+  static_assert(kScales0 + S * kScaleCols <= kTmemCols, "tensor memory");
   static_assert(kScales0 % 4 == 0 && kScaleCols % 4 == 0 && kColsA % 4 == 0, "where a scale matrix may begin");
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  uint64_t* bars = (uint64_t*)(smem + S * kStage);   // full[S], empty[S], acc_full[2], acc_empty[2], sc_full[2], sc_empty[2]
-  uint32_t* tmem_slot = (uint32_t*)(bars + 2 * S + 8);
+  // barriers: full[S], empty[S], of the accumulators full[2], empty[2], of the scales in shared memory the same
+  uint64_t* bars = (uint64_t*)(smem + S * kStage + kScaleStages * kScaleStage);
+  uint32_t* tmem_slot = (uint32_t*)(bars + 2 * S + 4 + 2 * kScaleStages);
   volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
-  Groups* groups = (Groups*)(bars + 2 * S + 10);
-  const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * S, accf0 = empty0 + 8 * S, acce0 = accf0 + 16, scf0 = acce0 + 16, sce0 = scf0 + 16;
+  Groups* groups = (Groups*)(tmem_slot + 2);
+  const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * S, accf0 = empty0 + 8 * S, acce0 = accf0 + 16;
+  const uint32_t ssf0 = acce0 + 16, sse0 = ssf0 + 8 * kScaleStages;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < S; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
-    for (int b = 0; b < 2; ++b) {
-      mbar_init(accf0 + 8 * b, 1); mbar_init(acce0 + 8 * b, kEpi);
-      mbar_init(scf0 + 8 * b, kScaleWarps); mbar_init(sce0 + 8 * b, 1);
-    }
+    for (int s = 0; s < S; ++s) { mbar_init(full0 + 8 * s, 1 + kScaleWarps); mbar_init(empty0 + 8 * s, 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(accf0 + 8 * b, 1); mbar_init(acce0 + 8 * b, kEpi); }
+    for (int b = 0; b < kScaleStages; ++b) { mbar_init(ssf0 + 8 * b, 1); mbar_init(sse0 + 8 * b, kScaleWarps); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (threadIdx.x == 32 * 2) { prefetch_map(&tmA); prefetch_map(&tmB); }
+  if (threadIdx.x == 32 * 2) { prefetch_map(&tmA); prefetch_map(&tmB); prefetch_map(&tmAs); prefetch_map(&tmBs); }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -123,7 +159,7 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   __syncthreads();
   tc_fence_after();
   chain_enter();
-  const uint32_t tmem_base = *tmem_slot, smem_base = smem_u32(smem);
+  const uint32_t tmem_base = *tmem_slot, smem_base = smem_u32(smem), scale_base = smem_base + S * kStage;
   // The first CTA clears the status word; another writes it two seconds into a wait at the earliest.
   if (blockIdx.x == 0 && threadIdx.x == 0) { p.status[0] = 0; p.status[1] = 0; }
   // The groups: offsets are the caller's memory, whatever they hold becomes rows inside [0, rows).
@@ -152,121 +188,112 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     for (int i = 0; i < kMaxE / 32; ++i) { run += tiles[i]; const int e = lane * (kMaxE / 32) + i; if (e < p.E) groups->first[e + 1] = run; }
   }
   __syncthreads();
-  const int total = groups->first[p.E] * p.tiles_m;
-  bool gave_up = false;
+  const int total = __shfl_sync(0xffffffffu, groups->first[p.E] * p.tiles_m, 0);
+  bool gave_up = tmem_base != 0;                     // cannot happen with all 512 columns taken; refuse rather than corrupt
+  if (gave_up && threadIdx.x == 0) { atomicExch(p.status + 1, 9); atomicExch(p.status, EC_ERR_TIMEOUT); }
 
-  if (warp == 0) {
+  if (gave_up) {
+    // nothing: fall through to the exit
+  } else if (warp == 0) {
     // ------------------------------------------------------------------ TMA
-    if (lane == 0) {
-      int stage = 0, e = 0; uint32_t phase = 0;
-      for (int tile = blockIdx.x; tile < total && !gave_up; tile += gridDim.x) {
-        const Tile t = find_tile<NT>(groups, p.tiles_m, tile, e);
-        for (int kb = 0; kb < p.kblocks; ++kb) {
-          if (!mbar_wait(empty0 + 8 * stage, phase ^ 1, abort_flag, p.status, 1)) { gave_up = true; break; }
-          const uint32_t sb = smem_base + stage * kStage, bar = full0 + 8 * stage;
-          mbar_expect_tx(bar, kStage);
-          tma_load_3d(sb, &tmB, bar, kb * kRowBytes, t.m * kM, t.e);
-          tma_load_2d(sb + kBBytes, &tmA, bar, kb * kRowBytes, t.row0);
-          if (++stage == S) { stage = 0; phase ^= 1; }
+    const uint32_t elected = elect_one();
+    uint32_t stage = 0, phase = 0, scale_stage = 0, scale_phase = 0, alive = 1;
+    int e = 0;
+    for (int tile = blockIdx.x; tile < total; tile += gridDim.x) {
+      Tile t = find_tile<NT>(groups, p.tiles_m, tile, e);
+      t.e = __shfl_sync(0xffffffffu, t.e, 0); t.m = __shfl_sync(0xffffffffu, t.m, 0); t.row0 = __shfl_sync(0xffffffffu, t.row0, 0);
+      for (int kb = 0; kb < p.kblocks; ++kb) {
+        if (kb % (kScaleStageK / kStageK) == 0) {
+          wait(alive, sse0 + 8 * scale_stage, scale_phase ^ 1, abort_flag, p.status, 7);
+          const uint32_t lead = elected & alive;
+          const uint32_t sc = scale_base + scale_stage * kScaleStage, bar = ssf0 + 8 * scale_stage;
+          expect_tx_if(lead, bar, kScaleStage);
+          tma_load_3d_if(lead, sc, &tmBs, bar, kb * (kStageK / 32), t.m * kM, t.e);
+          tma_load_2d_if(lead, sc + kM * kScaleRow, &tmAs, bar, kb * (kStageK / 32), t.row0);
+          if (++scale_stage == kScaleStages) { scale_stage = 0; scale_phase ^= 1; }
         }
+        wait(alive, empty0 + 8 * stage, phase ^ 1, abort_flag, p.status, 1);
+        const uint32_t lead = elected & alive;
+        const uint32_t sb = smem_base + stage * kStage, bar = full0 + 8 * stage;
+        expect_tx_if(lead, bar, kStage);
+        tma_load_3d_if(lead, sb, &tmB, bar, kb * kRowBytes, t.m * kM, t.e);
+        tma_load_2d_if(lead, sb + kBBytes, &tmA, bar, kb * kRowBytes, t.row0);
+        if (++stage == S) { stage = 0; phase ^= 1; }
       }
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA
-    if (lane == 0) {
-      // e2m1 operands, ue8m0 scales, NT columns, 128 rows; bits 4 and 29: which half of a scale column's four bytes (0 or 2)
-      const uint32_t idesc = (1u << 7) | (1u << 10) | ((uint32_t)(NT >> 3) << 17) | (1u << 23) | ((uint32_t)(kM >> 4) << 24);
-      int stage = 0, it = 0; uint32_t phase = 0, chunk = 0;
-      for (int tile = blockIdx.x; tile < total && !gave_up; tile += gridDim.x, ++it) {
-        const int buf = it & 1; const uint32_t use = (uint32_t)(it >> 1);
-        if (!mbar_wait(acce0 + 8 * buf, (use & 1) ^ 1, abort_flag, p.status, 2)) { gave_up = true; break; }
-        const uint32_t d = tmem_base + buf * NT;
-        for (int kb = 0; kb < p.kblocks; ++kb) {
-          const uint32_t sbuf = chunk & 1, scol = tmem_base + kScales0 + sbuf * kScaleCols;
-          if ((kb & 1) == 0 && !mbar_wait(scf0 + 8 * sbuf, (chunk >> 1) & 1, abort_flag, p.status, 3)) { gave_up = true; break; }
-          if (!mbar_wait(full0 + 8 * stage, phase, abort_flag, p.status, 4)) { gave_up = true; break; }
-          tc_fence_after();
-          const uint32_t sb = smem_base + stage * kStage, sa = sb + kBBytes;
-          const int steps = min(4, (p.blocks - 8 * kb + 1) / 2);     // MMAs that hold any of the contraction
+    // e2m1 operands, ue8m0 scales, NT columns, 128 rows; bits 4 and 29: which half of a scale column's four bytes (0 or 2)
+    constexpr uint32_t idesc = (1u << 7) | (1u << 10) | ((uint32_t)(NT >> 3) << 17) | (1u << 23) | ((uint32_t)(kM >> 4) << 24);
+    const uint32_t elected = elect_one(), low0 = desc_low(smem_base);
+    uint32_t stage = 0, phase = 0, it = 0, alive = 1;
+    for (int tile = blockIdx.x; tile < total; tile += gridDim.x, ++it) {
+      const uint32_t buf = it & 1, d = buf * NT;
+      wait(alive, acce0 + 8 * buf, ((it >> 1) & 1) ^ 1, abort_flag, p.status, 2);
+      for (int kb = 0; kb < p.kblocks; ++kb) {
+        wait(alive, full0 + 8 * stage, phase, abort_flag, p.status, 4);
+        tc_fence_after();
+        const uint32_t lead = elected & alive;
+        const uint32_t scales = kScales0 + stage * kScaleCols, blow = low0 + stage * (kStage >> 4), alow = blow + (kBBytes >> 4);
+        const int blocks = p.blocks - 8 * kb;        // left of the contraction; an MMA takes two
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (i < steps) {
-              const uint32_t g = 2 * (kb & 1) + (i >> 1), half = 2 * (i & 1);
-              tc_mma_mx(d, make_desc(sb + 32 * i, 16, 1024), make_desc(sa + 32 * i, 16, 1024), idesc | (half << 4) | (half << 29),
-                        scol + 4 * g, scol + 16 + kColsA * g, (kb | i) != 0);
-            }
-          }
-          tc_commit(empty0 + 8 * stage);
-          if (++stage == S) { stage = 0; phase ^= 1; }
-          if ((kb & 1) == 1 || kb + 1 == p.kblocks) { tc_commit(sce0 + 8 * sbuf); ++chunk; }
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t half = 2 * (i & 1);
+          tc_mma_mx_if(blocks > 2 * i ? lead : 0u, d, blow + 2 * i, alow + 2 * i, idesc | (half << 4) | (half << 29), scales + 4 * (i >> 1),
+                       scales + 8 + kColsA * (i >> 1), (kb | i) != 0);
         }
-        if (!gave_up) tc_commit(accf0 + 8 * buf);
+        tc_commit_if(lead, empty0 + 8 * stage);
+        if (++stage == S) { stage = 0; phase ^= 1; }
       }
+      tc_commit_if(elected & alive, accf0 + 8 * buf);
     }
   } else if (warp >= 2 + kEpi) {
     // ------------------------------------------------------------------ scales
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint8_t* asc = after_enter(p.a_scales);
-    const uint8_t* bsc = after_enter(p.b_scales);
-    const int chunks = (p.kblocks + 1) / 2, last = p.blocks - 16 * (chunks - 1);      // blocks of the last chunk
-    constexpr int kRowsA = NT / 32;
-    auto keep = [&](uint4 v) {                       // blocks behind the contraction's end: whatever lies there becomes 0, 2^-127
-      unsigned* w = reinterpret_cast<unsigned*>(&v);
+    constexpr int kRows = NT / 32;                   // of A, a lane's share of a tile; four of B
+    uint32_t scale_stage = 0, scale_phase = 0, stage = 0, phase = 0;
+    for (int tile = blockIdx.x; tile < total && !gave_up; tile += gridDim.x) {
+      for (int kb = 0; kb < p.kblocks; ++kb) {
+        const int part = kb % (kScaleStageK / kStageK);
+        if (part == 0 && !warp_wait(ssf0 + 8 * scale_stage, scale_phase, abort_flag, p.status, 8, lane)) { gave_up = true; break; }
+        // a row's eight bytes of this stage; the TMA unit's 32-byte swizzle exchanges the 16-byte halves of every other four rows
+        const uint32_t from = scale_base + scale_stage * kScaleStage + lane * kScaleRow + (((part >> 1) ^ ((lane >> 2) & 1)) << 4) + 8 * (part & 1);
+        uint32_t v[kScaleCols];                      // as they lie in tensor memory: B's first 128 of the contraction, its second, A's first, its second
 #pragma unroll
-      for (int g = 0; g < 4; ++g) { const int n = last - 4 * g; if (n < 4) w[g] = n <= 0 ? 0u : w[g] & (0xFFFFFFFFu >> (32 - 8 * n)); }
-      return v;
-    };
-    auto load = [&](const Tile& t, int c, uint4* b, uint4* a) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int col = t.m * kM + 32 * i + lane;
-        b[i] = col < p.N ? __ldg(reinterpret_cast<const uint4*>(bsc + ((int64_t)t.e * p.N + col) * p.scale_pitch + 16 * c)) : make_uint4(0, 0, 0, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < kRowsA; ++i) {
-        const int r = 32 * i + lane;
-        a[i] = r < t.rows ? __ldg(reinterpret_cast<const uint4*>(asc + (int64_t)(t.row0 + r) * p.scale_pitch + 16 * c)) : make_uint4(0, 0, 0, 0);
-      }
-      if (c + 1 == chunks) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) b[i] = keep(b[i]);
-#pragma unroll
-        for (int i = 0; i < kRowsA; ++i) a[i] = keep(a[i]);
-      }
-    };
-    int e = 0, tile = blockIdx.x, c = 0;
-    uint32_t chunk = 0;
-    uint4 b[4], a[kRowsA];
-    Tile t;
-    if (tile < total) { t = find_tile<NT>(groups, p.tiles_m, tile, e); load(t, 0, b, a); }
-    while (tile < total) {
-      const uint32_t sbuf = chunk & 1;
-      const bool ok = mbar_wait(sce0 + 8 * sbuf, ((chunk >> 1) & 1) ^ 1, abort_flag, p.status, 5);
-      if (!__all_sync(0xffffffffu, ok)) { gave_up = true; break; }
-      tc_fence_after();
-      const uint32_t col = tmem_base + lanes + kScales0 + sbuf * kScaleCols;
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        tc_st4(col + 4 * g, word(b[0], g), word(b[1], g), word(b[2], g), word(b[3], g));
-        const uint32_t ca = col + 16 + kColsA * g;
-        if constexpr (NT == 32) tc_st1(ca, word(a[0], g));
-        else if constexpr (NT == 64) tc_st2(ca, word(a[0], g), word(a[1], g));
-        else {
-          tc_st4(ca, word(a[0], g), word(a[1], g), word(a[2], g), word(a[3], g));
-          if constexpr (NT == 192) tc_st2(ca + 4, word(a[4], g), word(a[5], g));
+        for (int i = 0; i < 4 + kRows; ++i) {
+          const int at = i < 4 ? i : 4 + i, half = i < 4 ? 4 : kColsA;
+          asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v[at]), "=r"(v[at + half]) : "r"(from + 32 * i * kScaleRow) : "memory");
         }
+#pragma unroll
+        for (int i = kRows; i < kColsA; ++i) v[8 + i] = v[8 + kColsA + i] = 0;
+        const int blocks = p.blocks - 8 * kb;
+        if (blocks < 8) {                            // behind the contraction's end: whatever lies there becomes 0, 2^-127
+          const uint32_t first = blocks >= 4 ? 0xFFFFFFFFu : 0xFFFFFFFFu >> (32 - 8 * blocks), second = blocks > 4 ? 0xFFFFFFFFu >> (64 - 8 * blocks) : 0u;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) { v[i] &= first; v[4 + i] &= second; }
+#pragma unroll
+          for (int i = 0; i < kColsA; ++i) { v[8 + i] &= first; v[8 + kColsA + i] &= second; }
+        }
+        if (part == kScaleStageK / kStageK - 1 || kb + 1 == p.kblocks) {     // all of these scales are in registers
+          __syncwarp();
+          if (lane == 0) mbar_arrive(sse0 + 8 * scale_stage);
+          if (++scale_stage == kScaleStages) { scale_stage = 0; scale_phase ^= 1; }
+        }
+        if (!warp_wait(empty0 + 8 * stage, phase ^ 1, abort_flag, p.status, 5, lane)) { gave_up = true; break; }
+        tc_fence_after();
+        const uint32_t col = lanes + kScales0 + stage * kScaleCols;
+#pragma unroll
+        for (int i = 0; i < kScaleCols; i += 8) tc_st8(col + i, v + i);
+        tc_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(full0 + 8 * stage);
+        if (++stage == S) { stage = 0; phase ^= 1; }
       }
-      if (++c == chunks) { c = 0; tile += gridDim.x; if (tile < total) t = find_tile<NT>(groups, p.tiles_m, tile, e); }
-      if (tile < total) load(t, c, b, a);            // the next chunk's, while this one is used
-      tc_st_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(scf0 + 8 * sbuf);
-      ++chunk;
     }
   } else {
     // ------------------------------------------------------------------ epilogue
-    const int q = warp & 3;
+    const int q = warp & 3, first = 32 * ((warp - 2) >> 2);          // every other 32 rows
     int it = 0, e = 0;
     for (int tile = blockIdx.x; tile < total; tile += gridDim.x, ++it) {
       const Tile t = find_tile<NT>(groups, p.tiles_m, tile, e);
@@ -278,12 +305,11 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         const int64_t at = (int64_t)t.e * p.N + col;
         bias = p.bias_f32 ? __ldg((const float*)after_enter(p.bias) + at) : __bfloat162float(__ldg((const bf16*)after_enter(p.bias) + at));
       }
-      const bool ok = mbar_wait(accf0 + 8 * buf, use & 1, abort_flag, p.status, 6);
-      if (!__all_sync(0xffffffffu, ok)) { gave_up = true; break; }
+      if (!warp_wait(accf0 + 8 * buf, use & 1, abort_flag, p.status, 6, lane)) { gave_up = true; break; }
       tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + buf * NT;
 #pragma unroll 1
-      for (int c = 0; c < t.rows; c += 32) {         // uniform across the warp
+      for (int c = first; c < t.rows; c += 64) {     // uniform across the warp
         uint32_t r[32]; tc_ld32(taddr + c, r);
         float v[32];
 #pragma unroll
@@ -302,9 +328,16 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 #pragma unroll
           for (int j = 0; j < 32; ++j) if (in && j < left) out[(int64_t)j * p.N] = v[j];
         } else if constexpr (OUT == OUT_BF16) {
-          bf16* out = (bf16*)p.c + row * p.N + col;
+          // two rows at a time: even lanes take their column and the next one's of the first row, odd lanes of the second (N is even)
+          const int odd = lane & 1;
+          bf16* out = (bf16*)p.c + (row + odd) * p.N + (col - odd);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) if (in && j < left) out[(int64_t)j * p.N] = __float2bfloat16(v[j]);
+          for (int j = 0; j < 32; j += 2) {
+            const float got = __shfl_xor_sync(0xffffffffu, odd ? v[j] : v[j + 1], 1);
+            const __nv_bfloat162 pair = odd ? __floats2bfloat162_rn(got, v[j + 1]) : __floats2bfloat162_rn(v[j], got);
+            if (in && j + odd < left) *reinterpret_cast<__nv_bfloat162*>(out) = pair;
+            out += 2 * (int64_t)p.N;
+          }
         } else {
           // The warp's 32 columns are one block of every row: the largest magnitude by one reduction per row, eight rows' codes turned
           // between the lanes (lane 8 i + j ends with columns 8 i .. 8 i + 7 of row j).
@@ -354,28 +387,34 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   }
 }
 
-bool byte_map(CUtensorMap* tm, const void* base, int dims, int64_t inner, int64_t rows, int64_t batches, int box_rows) {
+bool byte_map(CUtensorMap* tm, const void* base, int dims, int64_t inner, int64_t rows, int64_t batches, int box_inner, int box_rows,
+              CUtensorMapSwizzle swizzle) {
   auto enc = (PFN_cuTensorMapEncodeTiled_v12000)tensor_map_encoder();
   if (!enc) return false;
   cuuint64_t size[3] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)batches};
   cuuint64_t strides[2] = {(cuuint64_t)inner, (cuuint64_t)(inner * rows)};
-  cuuint32_t box[3] = {kRowBytes, (cuuint32_t)box_rows, 1}, step[3] = {1, 1, 1};
+  cuuint32_t box[3] = {(cuuint32_t)box_inner, (cuuint32_t)box_rows, 1}, step[3] = {1, 1, 1};
   return enc(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, dims, const_cast<void*>(base), size, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+             swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int NT, int OUT>
 cudaError_t launch_one(const MxGemmArgs& g, MxParams p, int sms, cudaStream_t st) {
-  CUtensorMap ta, tb;
-  const int64_t inner = 16 * (int64_t)p.blocks;
-  if (!byte_map(&ta, g.A, 2, inner, g.rows, 1, NT) || !byte_map(&tb, g.B, 3, inner, g.N, g.E, kM)) return cudaErrorInvalidValue;
-  constexpr int smem = stages_of(NT) * (kBBytes + NT * kRowBytes) + 1024 + (2 * stages_of(NT) + 10) * 8 + (int)sizeof(Groups);
+  CUtensorMap ta, tb, tas, tbs;
+  const int64_t inner = 16 * (int64_t)p.blocks, pitch = 16 * (int64_t)((g.K + 511) / 512);
+  if (!byte_map(&ta, g.A, 2, inner, g.rows, 1, kRowBytes, NT, CU_TENSOR_MAP_SWIZZLE_128B) ||
+      !byte_map(&tb, g.B, 3, inner, g.N, g.E, kRowBytes, kM, CU_TENSOR_MAP_SWIZZLE_128B) ||
+      !byte_map(&tas, g.A_scales, 2, pitch, g.rows, 1, kScaleRow, NT, CU_TENSOR_MAP_SWIZZLE_32B) ||
+      !byte_map(&tbs, g.B_scales, 3, pitch, g.N, g.E, kScaleRow, kM, CU_TENSOR_MAP_SWIZZLE_32B)) return cudaErrorInvalidValue;
+  constexpr int smem = stages_of(NT) * (kBBytes + NT * kRowBytes) + kScaleStages * scale_stage_bytes(NT) + 1024 + (2 * stages_of(NT) + 5 + 2 * kScaleStages) * 8 +
+                       (int)sizeof(Groups);
+  static_assert(smem <= 227 * 1024, "shared memory");
   auto kern = gemm_mx_kernel<NT, OUT>;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   // no more CTAs than there can be tiles: every expert may add one that is not full
   const int64_t most = ((g.rows + NT - 1) / NT + (g.E < g.rows ? g.E : g.rows)) * p.tiles_m;
-  return launch_chained(kern, dim3((unsigned)(most < sms ? most : sms)), dim3(kThreads), smem, st, ta, tb, p);
+  return launch_chained(kern, dim3((unsigned)(most < sms ? most : sms)), dim3(kThreads), smem, st, ta, tb, tas, tbs, p);
 }
 template <int OUT>
 cudaError_t launch_out(const MxGemmArgs& g, const MxParams& p, int sms, cudaStream_t st) {
@@ -397,7 +436,6 @@ cudaError_t launch_gemm_mx(const MxGemmArgs& g, cudaStream_t st) {
   MxParams p; memset(&p, 0, sizeof(p));
   p.rows = g.rows; p.N = g.N; p.E = g.E; p.tiles_m = (g.N + kM - 1) / kM;
   p.blocks = (g.K + 31) / 32; p.kblocks = (p.blocks + 7) / 8; p.act = g.act; p.offsets = g.offsets;
-  p.a_scales = g.A_scales; p.b_scales = g.B_scales; p.scale_pitch = 16 * (int64_t)((g.K + 511) / 512);
   p.bias = g.bias; p.bias_f32 = g.bias_dtype == EC_F32; p.c = g.C; p.c_scales = g.C_scales;
   p.c_pitch = 16 * (int64_t)((g.N + 31) / 32); p.c_scale_pitch = 16 * (int64_t)((g.N + 511) / 512);
   p.status = g.status;
