@@ -16,7 +16,7 @@ namespace {
 // Up to kOnePiece choices one CTA does it all; beyond, a first launch leaves every CTA's counts and in the second each CTA sums
 // what it needs of them (148 x 256 counters at most, 148 KiB out of L2).
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kMaxExperts = 256;
-constexpr int64_t kOnePiece = 16384;
+constexpr int64_t kOnePiece = 4096;
 constexpr int kMaxPieces = 148;
 
 struct SortArgs {
@@ -191,11 +191,11 @@ template <typename T, int V> __device__ __forceinline__ typename Pack<T, V>::typ
   return p;
 }
 
-// KB rows of a token are on their way at a time; the sum runs over j in ascending order, in fp32, and is rounded once.
-template <typename T, typename TY, int G, int kPieces>
+// KB rows of a token are on their way at a time, kPieces pieces of each; the sum runs over j in ascending order, in fp32, and is rounded once.
+template <typename T, typename TY, int G, int kPieces, int KB>
 __global__ void __launch_bounds__(256) combine_rows_kernel(const uint4* Y, const float* weights, const int32_t* place, void* X_out, int64_t items,
                                                            int stretches, int pieces, int K, int64_t rows) {
-  constexpr int V = Vec<TY>::V, KB = 4;
+  constexpr int V = Vec<TY>::V;
   using Out = typename Pack<T, V>::type;
   chain_enter();
   const uint4* y = after_enter(Y);
@@ -239,12 +239,13 @@ __global__ void __launch_bounds__(256) combine_rows_kernel(const uint4* Y, const
   }
 }
 
-// A token is the work of WPT warps of a CTA: they share its pieces, so that dX_out is read once for KB of the token's rows, and the
-// dot products' parts are joined in a fixed order: lanes by halves, then the warps in turn.
-template <typename T, typename TY, int WPT>
+// A token is the work of G lanes, or of WPT warps of a CTA (G = 32): they share its pieces, so that dX_out is read once for KB of the
+// token's rows, and the dot products' parts are joined in a fixed order: lanes by halves, then the warps in turn.
+template <typename T, typename TY, int G, int WPT, int KB, int U>
 __global__ void __launch_bounds__(256) combine_backward_kernel(const void* dX_out, const uint4* Y, const float* weights, const int32_t* place, uint4* dY,
                                                                float* dweights, int64_t n, int pieces, int K, int64_t rows) {
-  constexpr int V = Vec<TY>::V, KB = 4, kTokens = 8 / WPT;
+  static_assert(G == 32 || WPT == 1, "lanes of a warp, or warps");
+  constexpr int V = Vec<TY>::V, kLanes = G * WPT, kTokens = 256 / kLanes;
   using In = typename Pack<T, V>::type;
   __shared__ float parts[8][KB];
   chain_enter();
@@ -252,9 +253,9 @@ __global__ void __launch_bounds__(256) combine_backward_kernel(const void* dX_ou
   const uint4* y = after_enter(Y);
   const float* ws = after_enter(weights);
   const int32_t* pl = after_enter(place);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % WPT;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x % G, sub = threadIdx.x % kLanes;
   for (int64_t t0 = (int64_t)blockIdx.x * kTokens; t0 < n; t0 += (int64_t)gridDim.x * kTokens) {       // the same for the whole CTA
-    const int64_t t = t0 + warp / WPT;
+    const int64_t t = t0 + threadIdx.x / kLanes;
     const bool live = t < n;
     for (int j0 = 0; j0 < K; j0 += KB) {
       int r[KB]; float w[KB], dot[KB];
@@ -266,41 +267,51 @@ __global__ void __launch_bounds__(256) combine_backward_kernel(const void* dX_ou
         dot[j] = 0.f;
       }
       if (live) {
-#pragma unroll 2
-        for (int p = sub * 32 + lane; p < pieces; p += WPT * 32) {
-          const In gp = __ldg(g + t * pieces + p);
-          uint4 v[KB];
+        for (int p0 = sub; p0 < pieces; p0 += kLanes * U) {
+          In gp[U]; uint4 v[U][KB];
 #pragma unroll
-          for (int j = 0; j < KB; ++j) if (r[j] >= 0) v[j] = __ldg(y + (int64_t)r[j] * pieces + p);
-          float a[V];
-          unpack<T, V>(gp, a);
+          for (int u = 0; u < U; ++u) {
+            const int p = p0 + u * kLanes;
+            if (p >= pieces) continue;
+            gp[u] = __ldg(g + t * pieces + p);
 #pragma unroll
-          for (int j = 0; j < KB; ++j) {
-            if (r[j] < 0) continue;
-            float f[V], o[V];
-            unpack<TY, V>(v[j], f);
+            for (int j = 0; j < KB; ++j) if (r[j] >= 0) v[u][j] = __ldg(y + (int64_t)r[j] * pieces + p);
+          }
 #pragma unroll
-            for (int i = 0; i < V; ++i) { dot[j] = fmaf(a[i], f[i], dot[j]); o[i] = w[j] * a[i]; }
-            dY[(int64_t)r[j] * pieces + p] = pack<TY, V>(o);
+          for (int u = 0; u < U; ++u) {
+            const int p = p0 + u * kLanes;
+            if (p >= pieces) continue;
+            float a[V];
+            unpack<T, V>(gp[u], a);
+#pragma unroll
+            for (int j = 0; j < KB; ++j) {
+              if (r[j] < 0) continue;
+              float f[V], o[V];
+              unpack<TY, V>(v[u][j], f);
+#pragma unroll
+              for (int i = 0; i < V; ++i) { dot[j] = fmaf(a[i], f[i], dot[j]); o[i] = w[j] * a[i]; }
+              dY[(int64_t)r[j] * pieces + p] = pack<TY, V>(o);
+            }
           }
         }
       }
 #pragma unroll
       for (int j = 0; j < KB; ++j)
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) dot[j] += __shfl_xor_sync(0xffffffffu, dot[j], o);
+        for (int o = G / 2; o > 0; o >>= 1) dot[j] += __shfl_xor_sync(0xffffffffu, dot[j], o);
       if constexpr (WPT == 1) {
-        if (live && lane < KB && j0 + lane < K) dweights[t * K + j0 + lane] = lane == 0 ? dot[0] : lane == 1 ? dot[1] : lane == 2 ? dot[2] : dot[3];
+#pragma unroll
+        for (int j = 0; j < KB; ++j) if (live && lane == j && j0 + j < K) dweights[t * K + j0 + j] = dot[j];
       } else {
         if (lane == 0)
 #pragma unroll
           for (int j = 0; j < KB; ++j) parts[warp][j] = dot[j];
         __syncthreads();
-        if (live && sub == 0 && lane < KB && j0 + lane < K) {
+        if (live && sub < KB && j0 + sub < K) {
           float sum = 0.f;
 #pragma unroll
-          for (int i = 0; i < WPT; ++i) sum += parts[warp + i][lane];
-          dweights[t * K + j0 + lane] = sum;
+          for (int i = 0; i < WPT; ++i) sum += parts[warp + i][sub];
+          dweights[t * K + j0 + sub] = sum;
         }
         __syncthreads();
       }
@@ -331,37 +342,47 @@ cudaError_t dispatch_with(const void* X, const int32_t* place, void* X_s, int64_
                         pieces, K, n * K);
 }
 
-template <typename T, typename TY, int G>
-cudaError_t combine_with(const void* Y, const float* w, const int32_t* place, void* X_out, int64_t n, int pieces, int K, int sms, cudaStream_t st) {
-  constexpr int kPieces = 2;
+template <typename T, typename TY, int G, int kPieces, int KB>
+cudaError_t combine_with(const void* Y, const float* w, const int32_t* place, void* X_out, int64_t n, int pieces, int K, cudaStream_t st) {
   const int stretches = (pieces + G * kPieces - 1) / (G * kPieces);
   const int64_t items = n * stretches;
-  return launch_chained(combine_rows_kernel<T, TY, G, kPieces>, dim3(item_grid(items, G, sms)), dim3(256), 0, st, (const uint4*)Y, w, place, X_out, items,
-                        stretches, pieces, K, n * K);
+  return launch_chained(combine_rows_kernel<T, TY, G, kPieces, KB>, dim3(item_grid(items, G, device_sms())), dim3(256), 0, st, (const uint4*)Y, w, place, X_out,
+                        items, stretches, pieces, K, n * K);
 }
+// Eight 16-byte loads on their way per lane where a row is long enough: two rows' four pieces or four rows' two.
 template <typename T, typename TY>
 cudaError_t combine_of(const void* Y, const float* w, const int32_t* place, void* X_out, int64_t n, int d, int K, cudaStream_t st) {
-  const int pieces = d / Vec<TY>::V, sms = device_sms();
+  const int pieces = d / Vec<TY>::V;
   switch (group_of(pieces)) {
-    case 32: return combine_with<T, TY, 32>(Y, w, place, X_out, n, pieces, K, sms, st);
-    case 16: return combine_with<T, TY, 16>(Y, w, place, X_out, n, pieces, K, sms, st);
-    default: return combine_with<T, TY, 8>(Y, w, place, X_out, n, pieces, K, sms, st);
+    case 8: return combine_with<T, TY, 8, 1, 4>(Y, w, place, X_out, n, pieces, K, st);
+    case 16: return combine_with<T, TY, 16, 1, 4>(Y, w, place, X_out, n, pieces, K, st);
   }
+  if (pieces <= 64) return combine_with<T, TY, 32, 2, 4>(Y, w, place, X_out, n, pieces, K, st);
+  return K <= 2 ? combine_with<T, TY, 32, 4, 2>(Y, w, place, X_out, n, pieces, K, st) : combine_with<T, TY, 32, 2, 4>(Y, w, place, X_out, n, pieces, K, st);
 }
 
-template <typename T, typename TY, int WPT>
+template <typename T, typename TY, int G, int WPT, int KB, int U>
 cudaError_t backward_with(const void* dX_out, const void* Y, const float* w, const int32_t* place, void* dY, float* dw, int64_t n, int pieces, int K,
-                          int sms, cudaStream_t st) {
-  const int64_t ctas = (n * WPT + 7) / 8, most = (int64_t)sms * 8;
-  return launch_chained(combine_backward_kernel<T, TY, WPT>, dim3((unsigned)(ctas < most ? ctas : most)), dim3(256), 0, st, dX_out, (const uint4*)Y, w, place,
-                        (uint4*)dY, dw, n, pieces, K, n * K);
+                          cudaStream_t st) {
+  const int64_t ctas = (n * G * WPT + 255) / 256, most = (int64_t)device_sms() * 8;
+  return launch_chained(combine_backward_kernel<T, TY, G, WPT, KB, U>, dim3((unsigned)(ctas < most ? ctas : most)), dim3(256), 0, st, dX_out, (const uint4*)Y, w,
+                        place, (uint4*)dY, dw, n, pieces, K, n * K);
+}
+template <typename T, typename TY, int KB, int U>
+cudaError_t backward_rows(const void* dX_out, const void* Y, const float* w, const int32_t* place, void* dY, float* dw, int64_t n, int pieces, int K,
+                          cudaStream_t st) {
+  switch (group_of(pieces)) {
+    case 8: return backward_with<T, TY, 8, 1, KB, 1>(dX_out, Y, w, place, dY, dw, n, pieces, K, st);
+    case 16: return backward_with<T, TY, 16, 1, KB, 1>(dX_out, Y, w, place, dY, dw, n, pieces, K, st);
+  }
+  if (pieces <= 64) return backward_with<T, TY, 32, 1, KB, U>(dX_out, Y, w, place, dY, dw, n, pieces, K, st);
+  if (pieces <= 256) return backward_with<T, TY, 32, 2, KB, U>(dX_out, Y, w, place, dY, dw, n, pieces, K, st);
+  return backward_with<T, TY, 32, 4, KB, U>(dX_out, Y, w, place, dY, dw, n, pieces, K, st);
 }
 template <typename T, typename TY>
 cudaError_t backward_of(const void* dX_out, const void* Y, const float* w, const int32_t* place, void* dY, float* dw, int64_t n, int d, int K, cudaStream_t st) {
-  const int pieces = d / Vec<TY>::V, sms = device_sms();
-  if (pieces <= 64) return backward_with<T, TY, 1>(dX_out, Y, w, place, dY, dw, n, pieces, K, sms, st);
-  if (pieces <= 128) return backward_with<T, TY, 2>(dX_out, Y, w, place, dY, dw, n, pieces, K, sms, st);
-  return backward_with<T, TY, 8>(dX_out, Y, w, place, dY, dw, n, pieces, K, sms, st);
+  const int pieces = d / Vec<TY>::V;
+  return K <= 2 ? backward_rows<T, TY, 2, 4>(dX_out, Y, w, place, dY, dw, n, pieces, K, st) : backward_rows<T, TY, 4, 2>(dX_out, Y, w, place, dY, dw, n, pieces, K, st);
 }
 
 }  // namespace
