@@ -75,16 +75,19 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* X, int64_t 
       q[h] = quantize8(x[h], s[h]);
       s[h] = gather_scales<L>(s[h], lane);
     }
+    unsigned word = 0;                               // L = 32: lane i takes word i of the stretch's 2 H scale words, one store for all
+    if constexpr (L == 32) {
+#pragma unroll
+      for (int h = 0; h < H; ++h) { const unsigned w = __shfl_sync(0xffffffffu, s[h], 16 * (lane & 1)); if (lane >> 1 == h) word = w; }
+    }
     auto store = [&](int64_t r) {
 #pragma unroll
-      for (int h = 0; h < H; ++h) {
-        const int c = c0 + 256 * h;
-        if (c < 32 * blocks) *reinterpret_cast<unsigned*>(codes + r * code_pitch + c / 2) = q[h];
-        if constexpr (L == 32) {
-          if ((lane & 15) == 0 && c < 512 * groups) *reinterpret_cast<unsigned*>(scales + r * scale_pitch + c / 32) = s[h];
-        } else {
-          if (lane % L == 0) *reinterpret_cast<uint4*>(scales + r * scale_pitch) = make_uint4(s[h], 0, 0, 0);
-        }
+      for (int h = 0; h < H; ++h) if (c0 + 256 * h < 32 * blocks) *reinterpret_cast<unsigned*>(codes + r * code_pitch + (c0 + 256 * h) / 2) = q[h];
+      if constexpr (L == 32) {
+        const int at = (c0 - 8 * lane) / 32 + 4 * lane;
+        if (lane < 2 * H && at < 16 * groups) *reinterpret_cast<unsigned*>(scales + r * scale_pitch + at) = word;
+      } else {
+        if (lane % L == 0) *reinterpret_cast<uint4*>(scales + r * scale_pitch) = make_uint4(s[0], 0, 0, 0);
       }
     };
     if (!live) continue;                             // no lane of the warp is waited for below
@@ -104,7 +107,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* X, int64_t 
 // 64 columns; a warp one block of 32 of the contraction, lane i two neighbouring columns, so its 32 loads are 32 lines.  The codes
 // turn in shared memory and leave as 128 bytes of an output row at a time.
 template <typename T>
-__global__ void __launch_bounds__(256) quantize_columns_kernel(const T* X, int rows, int cols, int groups, uint8_t* codes, uint8_t* scales) {
+__global__ void __launch_bounds__(256, 3) quantize_columns_kernel(const T* X, int rows, int cols, int groups, uint8_t* codes, uint8_t* scales) {
   __shared__ uint4 tile[64][8 + 1];
   __shared__ __align__(8) uint8_t tile_scales[64][8];
   chain_enter();
@@ -155,46 +158,50 @@ __global__ void __launch_bounds__(256) quantize_columns_kernel(const T* X, int r
     *reinterpret_cast<uint2*>(scales + (out0 + threadIdx.x) * (16 * (int64_t)groups) + b0) = *reinterpret_cast<const uint2*>(tile_scales[threadIdx.x]);
 }
 
-// A thread turns a word of eight codes into eight values, four words at a time, each a whole line of the warp's.
-template <typename T>
-__global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* codes, const uint8_t* scales, int64_t words, int words_per_row, int cols, int blocks,
-                                                         int scale_pitch, T* X) {
+// The codes of 16 bytes of values at a time: eight in bf16, four in fp32, so that a warp's stores are whole lines.  The three bits of a
+// magnitude, put where fp32 has the end of its exponent and the start of its fraction, are 2^-126 times what they stand for, the
+// subnormal ones among them.  Lanes as in the quantisation: L = 32, U times 32 pieces of a row; else 32 / L rows, U times.
+template <typename T, int L, int U>
+__global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t items, int stretches, int pieces,
+                                                         int code_pitch, int scale_pitch, uint4* X) {
+  constexpr int V = 16 / sizeof(T);
+  using Codes = typename std::conditional<V == 8, unsigned, unsigned short>::type;
   chain_enter();
-  const unsigned* q = reinterpret_cast<const unsigned*>(after_enter(codes));
+  const uint8_t* q = after_enter(codes);
   const uint8_t* sc = after_enter(scales);
-  constexpr int U = 4;
-  for (int64_t i0 = (int64_t)blockIdx.x * (256 * U) + threadIdx.x; i0 < words; i0 += (int64_t)gridDim.x * (256 * U)) {
-    unsigned v[U]; unsigned s[U]; int64_t at[U]; int col[U];
+  const int lane = threadIdx.x & 31;
+  for (int64_t it = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 5; it < items; it += (int64_t)gridDim.x * 8) {
+    const int64_t first = L == 32 ? it / stretches : it * (32 / L * U);
+    const int w0 = L == 32 ? (int)(it - first * stretches) * (32 * U) : 0;
+    unsigned v[U], s[U];
+    bool live[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t i = i0 + 256 * u, row = i / words_per_row;
-      const int w = (int)(i - row * words_per_row);
-      col[u] = 8 * w; at[u] = row * cols + 8 * w;
-      if (i < words) { v[u] = __ldg(q + row * (4 * (int64_t)blocks) + w); s[u] = __ldg(sc + row * scale_pitch + w / 4); }
+      const int64_t row = L == 32 ? first : first + u * (32 / L) + lane / L;
+      const int w = L == 32 ? w0 + 32 * u + lane : lane % L;
+      live[u] = w < pieces && row < rows;
+      if (live[u]) { v[u] = __ldg(reinterpret_cast<const Codes*>(q + row * code_pitch) + w); s[u] = __ldg(sc + row * scale_pitch + w * V / 32); }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (i0 + 256 * u >= words) break;
+      if (!live[u]) continue;
+      const int64_t row = L == 32 ? first : first + u * (32 / L) + lane / L;
+      const int w = L == 32 ? w0 + 32 * u + lane : lane % L;
       const float p = mx_scale_value(s[u]);
-      float f[8];
+      float f[V];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const unsigned code = v[u] >> (4 * j), e = (code >> 1) & 3, m = code & 1;
-        // 1.m x 2^(e - 1), or m / 2 where e is 0, in fp32's fields
-        const unsigned bits = (e == 0 ? m * 0x3F000000u : ((126u + e) << 23) | (m << 22)) | ((code & 8) << 28);
-        f[j] = __uint_as_float(bits) * p;
+      for (int j = 0; j < V; ++j) {
+        const unsigned bits = (4 * j <= 22 ? v[u] << ((22 - 4 * j) & 31) : v[u] >> ((4 * j - 22) & 31)) & 0x01C00000u;
+        f[j] = __uint_as_float(bits | ((v[u] << (28 - 4 * j)) & 0x80000000u)) * 0x1p126f * p;
       }
-      T* out = X + at[u];
-      if constexpr (sizeof(T) == 2) {
-        uint4 o;
-        unsigned* ow = reinterpret_cast<unsigned*>(&o);
+      uint4 o;
+      unsigned* ow = reinterpret_cast<unsigned*>(&o);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) { __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]); ow[j] = *reinterpret_cast<unsigned*>(&h); }
-        *reinterpret_cast<uint4*>(out) = o;
-      } else {
-        *reinterpret_cast<float4*>(out) = make_float4(f[0], f[1], f[2], f[3]);
-        if (col[u] + 4 < cols) *reinterpret_cast<float4*>(out + 4) = make_float4(f[4], f[5], f[6], f[7]);
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (V == 8) { __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]); ow[j] = *reinterpret_cast<unsigned*>(&h); }
+        else ow[j] = __float_as_uint(f[j]);
       }
+      X[row * pieces + w] = o;
     }
   }
 }
@@ -205,8 +212,8 @@ int sm_count() {
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   return sms;
 }
-unsigned grid_of(int64_t ctas) {
-  const int64_t most = (int64_t)sm_count() * 16;
+unsigned grid_of(int64_t ctas, int per_sm) {
+  const int64_t most = (int64_t)sm_count() * per_sm;
   return (unsigned)(ctas < most ? ctas : most);
 }
 
@@ -214,7 +221,7 @@ template <typename T, bool PLACED, int L, int H>
 cudaError_t rows_with(const T* X, int64_t rows, int cols, uint8_t* codes, uint8_t* scales, const int32_t* place, int K, cudaStream_t st) {
   const int stretches = L == 32 ? (cols + 256 * H - 1) / (256 * H) : 1;
   const int64_t items = L == 32 ? rows * stretches : (rows + 32 / L - 1) / (32 / L);
-  return launch_chained(quantize_rows_kernel<T, PLACED, L, H>, dim3(grid_of((items + 7) / 8)), dim3(256), 0, st, X, rows, items, stretches, cols, codes, scales,
+  return launch_chained(quantize_rows_kernel<T, PLACED, L, H>, dim3(grid_of((items + 7) / 8, 16)), dim3(256), 0, st, X, rows, items, stretches, cols, codes, scales,
                         place, K, rows * K);
 }
 template <typename T, bool PLACED>
@@ -251,12 +258,27 @@ cudaError_t launch_mx_dispatch(int dtype, const void* X, const int32_t* place, i
   return dtype == 0 ? rows_of<float, true>((const float*)X, n, d, codes, scales, place, K, st) : rows_of<bf16, true>((const bf16*)X, n, d, codes, scales, place, K, st);
 }
 
+namespace {
+template <typename T, int L, int U>
+cudaError_t dequantize_with(const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols, int pieces, void* X, cudaStream_t st) {
+  const int stretches = L == 32 ? (pieces + 32 * U - 1) / (32 * U) : 1;
+  const int64_t items = L == 32 ? rows * stretches : (rows + 32 / L * U - 1) / (32 / L * U);
+  return launch_chained(dequantize_kernel<T, L, U>, dim3(grid_of((items + 7) / 8, 64)), dim3(256), 0, st, codes, scales, rows, items, stretches, pieces,
+                        16 * ((cols + 31) / 32), 16 * ((cols + 511) / 512), (uint4*)X);
+}
+template <typename T>
+cudaError_t dequantize_of(const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols, void* X, cudaStream_t st) {
+  const int pieces = cols / (16 / (int)sizeof(T));
+  if (pieces <= 4) return dequantize_with<T, 4, 2>(codes, scales, rows, cols, pieces, X, st);
+  if (pieces <= 8) return dequantize_with<T, 8, 2>(codes, scales, rows, cols, pieces, X, st);
+  if (pieces <= 16) return dequantize_with<T, 16, 2>(codes, scales, rows, cols, pieces, X, st);
+  if (pieces <= 32) return dequantize_with<T, 32, 1>(codes, scales, rows, cols, pieces, X, st);
+  return pieces <= 64 ? dequantize_with<T, 32, 2>(codes, scales, rows, cols, pieces, X, st) : dequantize_with<T, 32, 4>(codes, scales, rows, cols, pieces, X, st);
+}
+}  // namespace
+
 cudaError_t launch_mx_dequantize(int dtype, const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols, void* X, cudaStream_t st) {
-  const int per_row = (cols + 7) / 8, blocks = (cols + 31) / 32, pitch = 16 * ((cols + 511) / 512);
-  const int64_t words = rows * per_row;
-  const dim3 grid(grid_of((words + 1023) / 1024));
-  if (dtype == 0) return launch_chained(dequantize_kernel<float>, grid, dim3(256), 0, st, codes, scales, words, per_row, cols, blocks, pitch, (float*)X);
-  return launch_chained(dequantize_kernel<bf16>, grid, dim3(256), 0, st, codes, scales, words, per_row, cols, blocks, pitch, (bf16*)X);
+  return dtype == 0 ? dequantize_of<float>(codes, scales, rows, cols, X, st) : dequantize_of<bf16>(codes, scales, rows, cols, X, st);
 }
 
 }  // namespace ecmoe

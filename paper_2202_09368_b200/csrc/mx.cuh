@@ -17,6 +17,8 @@ __device__ __forceinline__ unsigned mx_scale_of(unsigned amax_bits) {
 // 2^(127 - s), by which the block's values are multiplied: exact, also where a value is subnormal (2^127 is its largest).  A NaN block's
 // values become zeros of either sign or NaN here and mx_codes is not asked for them.
 __device__ __forceinline__ float mx_inverse(unsigned s) { return __uint_as_float((254u - s) << 23); }
+// The same straight from the largest magnitude's bits: 256 - e in the exponent's place, at most 254
+__device__ __forceinline__ float mx_inverse_of(unsigned amax_bits) { return __uint_as_float(min(0x80000000u - (amax_bits & 0x7F800000u), 0x7F000000u)); }
 // 2^(s - 127); s = 0 is subnormal
 __device__ __forceinline__ float mx_scale_value(unsigned s) {
   return __uint_as_float(s == kMxNan ? 0x7fffffffu : s == 0 ? 0x00400000u : s << 23);

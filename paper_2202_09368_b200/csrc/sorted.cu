@@ -329,7 +329,7 @@ int device_sms() {
 // Lanes per stretch: a warp for rows of 32 pieces and more
 int group_of(int pieces) { return pieces > 16 ? 32 : pieces > 8 ? 16 : 8; }
 unsigned item_grid(int64_t items, int group, int sms) {
-  const int64_t ctas = (items * group + 255) / 256, most = (int64_t)sms * 16;
+  const int64_t ctas = (items * group + 255) / 256, most = (int64_t)sms * 64;
   return (unsigned)(ctas < most ? ctas : most);
 }
 
@@ -349,7 +349,9 @@ cudaError_t combine_with(const void* Y, const float* w, const int32_t* place, vo
   return launch_chained(combine_rows_kernel<T, TY, G, kPieces, KB>, dim3(item_grid(items, G, device_sms())), dim3(256), 0, st, (const uint4*)Y, w, place, X_out,
                         items, stretches, pieces, K, n * K);
 }
-// Eight 16-byte loads on their way per lane where a row is long enough: two rows' four pieces or four rows' two.
+// Four 16-byte loads on their way per lane: the pieces of one row, of two, or one piece of four (measured against twice as many, which
+// cost the registers of a third of the warps: 16384 x 4096 bf16, two rows per token, 68 us and 77; 65536 x 1024, eight rows, 194 and 209;
+// 4096 x 8192, one row, four pieces 25.6, two 33.6).
 template <typename T, typename TY>
 cudaError_t combine_of(const void* Y, const float* w, const int32_t* place, void* X_out, int64_t n, int d, int K, cudaStream_t st) {
   const int pieces = d / Vec<TY>::V;
@@ -357,8 +359,8 @@ cudaError_t combine_of(const void* Y, const float* w, const int32_t* place, void
     case 8: return combine_with<T, TY, 8, 1, 4>(Y, w, place, X_out, n, pieces, K, st);
     case 16: return combine_with<T, TY, 16, 1, 4>(Y, w, place, X_out, n, pieces, K, st);
   }
-  if (pieces <= 64) return combine_with<T, TY, 32, 2, 4>(Y, w, place, X_out, n, pieces, K, st);
-  return K <= 2 ? combine_with<T, TY, 32, 4, 2>(Y, w, place, X_out, n, pieces, K, st) : combine_with<T, TY, 32, 2, 4>(Y, w, place, X_out, n, pieces, K, st);
+  if (K == 1) return combine_with<T, TY, 32, 4, 1>(Y, w, place, X_out, n, pieces, K, st);
+  return K == 2 ? combine_with<T, TY, 32, 2, 2>(Y, w, place, X_out, n, pieces, K, st) : combine_with<T, TY, 32, 1, 4>(Y, w, place, X_out, n, pieces, K, st);
 }
 
 template <typename T, typename TY, int G, int WPT, int KB, int U>
