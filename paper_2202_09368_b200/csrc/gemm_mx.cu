@@ -51,6 +51,9 @@ __host__ __device__ constexpr int stages_of(int nt) {
 __host__ __device__ constexpr int cols_a(int nt) { return nt <= 128 ? 4 : 8; }
 __host__ __device__ constexpr int scale_cols(int nt) { return 8 + 2 * cols_a(nt); }
 
+// TMA boxes a stage's rows of A come in
+__host__ __device__ constexpr int boxes_of(int nt) { return nt >= 128 ? 2 : 1; }
+
 struct MxParams {
   int64_t rows;
   int N, E, tiles_m, blocks, kblocks;                // blocks: of 32 along the contraction; kblocks: stages of 256
@@ -170,6 +173,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmAs,
                const __grid_constant__ CUtensorMap tmBs, const MxParams p) {
   constexpr int S = stages_of(NT), kStage = kBBytes + NT * kRowBytes, kScaleStage = scale_stage_bytes(NT);
+  constexpr int kBoxes = boxes_of(NT), kBoxBytes = NT / kBoxes * kRowBytes;
   constexpr int kColsA = cols_a(NT), kScaleCols = scale_cols(NT), kScales0 = 2 * NT;
   static_assert(kScales0 + S * kScaleCols <= kTmemCols, "tensor memory");
   static_assert(kScales0 % 4 == 0 && kScaleCols % 4 == 0 && kColsA % 4 == 0, "where a scale matrix may begin");
@@ -236,10 +240,11 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     // ------------------------------------------------------------------ TMA
     const uint32_t elected = elect_one();
     uint32_t stage = 0, phase = 0, scale_stage = 0, scale_phase = 0, alive = 1;
-    Walk<NT> walk(groups, p.tiles_m);
+    Walk<NT> walk(groups, p.tiles_m);                // of A only the halves of a tile that hold rows are loaded
     for (int tile = blockIdx.x, step = 0; tile < total; tile += gridDim.x, step = gridDim.x) {
       walk.next(step);
       const int e = __shfl_sync(0xffffffffu, walk.e, 0), col0 = __shfl_sync(0xffffffffu, walk.m, 0) * kM, row0 = __shfl_sync(0xffffffffu, walk.row0, 0);
+      const int boxes = __shfl_sync(0xffffffffu, walk.rows > NT / kBoxes ? kBoxes : 1, 0);
       for (int kb = 0; kb < p.kblocks; ++kb) {
         if (kb % (kScaleStageK / kStageK) == 0) {
           wait(alive, sse0 + 8 * scale_stage, scale_phase ^ 1, abort_flag, p.status, 7);
@@ -253,19 +258,23 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         wait(alive, empty0 + 8 * stage, phase ^ 1, abort_flag, p.status, 1);
         const uint32_t lead = elected & alive;
         const uint32_t sb = smem_base + stage * kStage, bar = full0 + 8 * stage;
-        expect_tx_if(lead, bar, kStage);
+        expect_tx_if(lead, bar, kBBytes + boxes * kBoxBytes);
         tma_load_3d_if(lead, sb, &tmB, bar, kb * kRowBytes, col0, e);
         tma_load_2d_if(lead, sb + kBBytes, &tmA, bar, kb * kRowBytes, row0);
+        if constexpr (kBoxes == 2) tma_load_2d_if(boxes == 2 ? lead : 0u, sb + kBBytes + kBoxBytes, &tmA, bar, kb * kRowBytes, row0 + NT / 2);
         if (++stage == S) { stage = 0; phase ^= 1; }
       }
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA
-    // e2m1 operands, ue8m0 scales, NT columns, 128 rows; bits 4 and 29: which half of a scale column's four bytes (0 or 2)
-    constexpr uint32_t idesc = (1u << 7) | (1u << 10) | ((uint32_t)(NT >> 3) << 17) | (1u << 23) | ((uint32_t)(kM >> 4) << 24);
+    // e2m1 operands, ue8m0 scales, 128 rows, as many columns as the tile has rows of A, in 32s; bits 4 and 29: which half of a scale column's four bytes (0 or 2)
+    constexpr uint32_t idesc0 = (1u << 7) | (1u << 10) | (1u << 23) | ((uint32_t)(kM >> 4) << 24);
     const uint32_t elected = elect_one(), low0 = desc_low(smem_base);
     uint32_t stage = 0, phase = 0, it = 0, alive = 1;
-    for (int tile = blockIdx.x; tile < total; tile += gridDim.x, ++it) {
+    Walk<NT> walk(groups, p.tiles_m);
+    for (int tile = blockIdx.x, step = 0; tile < total; tile += gridDim.x, step = gridDim.x, ++it) {
+      walk.next(step);
+      const uint32_t idesc = __shfl_sync(0xffffffffu, idesc0 | ((uint32_t)(walk.rows + 31) / 32 << 19), 0);
       const uint32_t buf = it & 1, d = buf * NT;
       wait(alive, acce0 + 8 * buf, ((it >> 1) & 1) ^ 1, abort_flag, p.status, 2);
       for (int kb = 0; kb < p.kblocks; ++kb) {
@@ -445,7 +454,7 @@ template <int NT, int OUT>
 cudaError_t launch_one(const MxGemmArgs& g, MxParams p, int sms, cudaStream_t st) {
   CUtensorMap ta, tb, tas, tbs;
   const int64_t inner = 16 * (int64_t)p.blocks, pitch = 16 * (int64_t)((g.K + 511) / 512);
-  if (!byte_map(&ta, g.A, 2, inner, g.rows, 1, kRowBytes, NT, CU_TENSOR_MAP_SWIZZLE_128B) ||
+  if (!byte_map(&ta, g.A, 2, inner, g.rows, 1, kRowBytes, NT / boxes_of(NT), CU_TENSOR_MAP_SWIZZLE_128B) ||
       !byte_map(&tb, g.B, 3, inner, g.N, g.E, kRowBytes, kM, CU_TENSOR_MAP_SWIZZLE_128B) ||
       !byte_map(&tas, g.A_scales, 2, pitch, g.rows, 1, kScaleRow, NT, CU_TENSOR_MAP_SWIZZLE_32B) ||
       !byte_map(&tbs, g.B_scales, 3, pitch, g.N, g.E, kScaleRow, kM, CU_TENSOR_MAP_SWIZZLE_32B)) return cudaErrorInvalidValue;
@@ -466,6 +475,7 @@ cudaError_t launch_out(const MxGemmArgs& g, const MxParams& p, int sms, cudaStre
   // choices spread by exp(normal / 2), us for 64, 128, 192: a mean of 32 rows 425, 418, 459; 64 rows 543, 469, 503; 128 rows 839, 619, 598;
   // 256 rows 1510, 964, 843; 512 rows 2921, 1623, 1377; sixteen rows, 1024 x 1024: 15.5, 17.3, 19.2.
   const int64_t mean = g.rows / g.E;
+  if (mean <= 2) return launch_one<32, OUT>(g, p, sms, st);        // eight rows of one token each: 64 us, with tiles of 64 rows 72 (more of the weights on their way)
   if (mean <= 20) return launch_one<64, OUT>(g, p, sms, st);
   return mean <= 90 ? launch_one<128, OUT>(g, p, sms, st) : launch_one<192, OUT>(g, p, sms, st);
 }
