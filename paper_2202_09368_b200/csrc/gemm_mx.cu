@@ -14,6 +14,8 @@
 //   warps 14-17  scales: a stage's from shared through registers into tensor memory, where every quarter of the lanes wants its own
 //                copy: row 32 c + l of a tile in lane l, column c, four blocks' bytes to a column.  Rows start anywhere, so no
 //                prepared layout could serve them.
+// Few rows leave few tiles: then a cluster of CTAs shares each (SPLIT), each a stretch of the contraction, and the first adds up the others'
+// accumulators, which they write into its shared memory, in the order of the stretches.
 // Two accumulators of NT columns, and as many buffers of scales as there are stages: a stage is full when its operands have landed and
 // its scales are in tensor memory, and one commit frees both.  (A wait that is over at once still takes the MMA warp 100 cycles, a commit
 // 60 to 100, issuing an MMA 80: with barriers of their own for the scales a stage took 815 cycles beside the MMAs' 384.)
@@ -42,8 +44,11 @@ constexpr int kScaleStages = 2, kScaleStageK = 1024, kScaleRow = kScaleStageK / 
 constexpr int kSmemBudget = 221 * 1024;
 
 __host__ __device__ constexpr int scale_stage_bytes(int nt) { return (kM + nt) * kScaleRow; }
-__host__ __device__ constexpr int stages_of(int nt) {
-  const int fit = (kSmemBudget - kScaleStages * scale_stage_bytes(nt)) / (kBBytes + nt * kRowBytes);
+// Most CTAs to a tile, and what the first of them keeps for the others' accumulators
+__host__ __device__ constexpr int most_split(int nt) { return nt == 32 ? 4 : nt == 64 ? 2 : 1; }
+__host__ __device__ constexpr int parts_bytes(int nt, bool split) { return split ? (most_split(nt) - 1) * kM * nt * 4 : 0; }
+__host__ __device__ constexpr int stages_of(int nt, bool split) {
+  const int fit = (kSmemBudget - parts_bytes(nt, split) - kScaleStages * scale_stage_bytes(nt)) / (kBBytes + nt * kRowBytes);
   return fit > 10 ? 10 : fit;
 }
 // Columns of tensor memory for 128 of the contraction of A's scales, and for a stage's of both.  tcgen05.mma wants a scale matrix to begin
@@ -57,7 +62,7 @@ __host__ __device__ constexpr int boxes_of(int nt) { return nt >= 128 ? 2 : 1; }
 struct MxParams {
   int64_t rows;
   int N, E, tiles_m, blocks, kblocks;                // blocks: of 32 along the contraction; kblocks: stages of 256
-  int act;
+  int act, split;                                    // split: CTAs to a tile
   const int32_t* offsets;
   const void* bias; int bias_f32;
   void* c; uint8_t* c_scales; int64_t c_pitch, c_scale_pitch;     // c_pitch in bytes
@@ -104,11 +109,44 @@ __device__ __forceinline__ void tc_mma_mx_if(uint32_t lead, uint32_t d, uint32_t
                " @q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, %3, [%4], [%5], p;\n}\n"
                ::"r"(d), "r"(alow), "r"(blow), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate), "r"(lead), "n"(kDescHigh) : "memory");
 }
+// What another CTA of the cluster wrote before it arrived: acquire at the cluster's scope.  Gives up like mbar_wait.
+__device__ __forceinline__ bool cluster_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int where, int lane) {
+  bool ok = true;
+  if (lane == 0) {
+    auto done = [&] {
+      uint32_t r;
+      asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+                   : "=r"(r) : "r"(bar), "r"(parity) : "memory");
+      return r != 0;
+    };
+    if (!done()) {
+      const unsigned long long t0 = globaltimer();
+      for (uint32_t spin = 1; !done(); ++spin) {
+        if ((spin & 63u) != 0) continue;
+        if (*abort_flag) { ok = false; break; }
+        if (globaltimer() - t0 > kWaitNs) {
+          *abort_flag = 1;
+          atomicExch(status + 1, where); atomicExch(status, EC_ERR_TIMEOUT);
+          ok = false;
+          break;
+        }
+      }
+    }
+  }
+  ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+  __syncwarp();                                      // what the lane has seen the others see
+  return ok;
+}
+__device__ __forceinline__ void st_cluster4(uint32_t addr, const float* v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]) : "memory");
+}
 // A warp's wait with an answer: one lane polls.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int where, int lane) {
   bool ok = true;
   if (lane == 0) ok = mbar_wait(bar, parity, abort_flag, status, where);
-  return __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+  ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+  __syncwarp();                                      // what the lane has seen the others see
+  return ok;
 }
 __device__ __forceinline__ void tc_st8(uint32_t taddr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
@@ -142,13 +180,13 @@ struct Groups {
   int tiles[kMaxE];                                  // row tiles
   int active, total;                                 // experts; tiles in all
 };
-// A role's walk through the CTA's tiles: tile, tile + gridDim.x, ... without a division but by the row tiles of the expert at hand.
+// A role's walk through the CTA's tiles, the first and every so many from there on, without a division but by the row tiles of the expert at hand.
 template <int NT>
 struct Walk {
   const Groups* g; int tiles_m;
   int i, left, n; float inv;                         // expert number i of the list, place inside its tiles, its row tiles and their inverse
   int e, m, row0, rows;                              // the tile at hand
-  __device__ __forceinline__ Walk(const Groups* groups, int m) : g(groups), tiles_m(m), i(-1), left((int)blockIdx.x), n(0) {}
+  __device__ __forceinline__ Walk(const Groups* groups, int m, int first) : g(groups), tiles_m(m), i(-1), left(first), n(0) {}
   // moves on by `step` tiles (0 for the first); false behind the last
   __device__ __forceinline__ bool next(int step) {
     left += step;
@@ -168,11 +206,11 @@ struct Walk {
   }
 };
 
-template <int NT, int OUT>
+template <int NT, int OUT, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1)
 gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmAs,
                const __grid_constant__ CUtensorMap tmBs, const MxParams p) {
-  constexpr int S = stages_of(NT), kStage = kBBytes + NT * kRowBytes, kScaleStage = scale_stage_bytes(NT);
+  constexpr int S = stages_of(NT, SPLIT), kStage = kBBytes + NT * kRowBytes, kScaleStage = scale_stage_bytes(NT);
   constexpr int kBoxes = boxes_of(NT), kBoxBytes = NT / kBoxes * kRowBytes;
   constexpr int kColsA = cols_a(NT), kScaleCols = scale_cols(NT), kScales0 = 2 * NT;
   static_assert(kScales0 + S * kScaleCols <= kTmemCols, "tensor memory");
@@ -180,18 +218,26 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   // barriers: full[S], empty[S], of the accumulators full[2], empty[2], of the scales in shared memory the same
-  uint64_t* bars = (uint64_t*)(smem + S * kStage + kScaleStages * kScaleStage);
-  uint32_t* tmem_slot = (uint32_t*)(bars + 2 * S + 4 + 2 * kScaleStages);
+  // and, of the parts of a split tile, full and empty
+  uint64_t* bars = (uint64_t*)(smem + S * kStage + kScaleStages * kScaleStage + parts_bytes(NT, SPLIT));
+  uint32_t* tmem_slot = (uint32_t*)(bars + 2 * S + 6 + 2 * kScaleStages);
   volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
   Groups* groups = (Groups*)(tmem_slot + 2);
   const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * S, accf0 = empty0 + 8 * S, acce0 = accf0 + 16;
-  const uint32_t ssf0 = acce0 + 16, sse0 = ssf0 + 8 * kScaleStages;
+  const uint32_t ssf0 = acce0 + 16, sse0 = ssf0 + 8 * kScaleStages, partf = sse0 + 8 * kScaleStages, parte = partf + 8;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // a cluster's CTAs take the same tiles, each a stretch of whole scale stages of the contraction
+  const int ctas = SPLIT ? p.split : 1, rank = SPLIT ? (int)blockIdx.x % ctas : 0;
+  const int first_tile = SPLIT ? blockIdx.x / ctas : blockIdx.x, tile_step = SPLIT ? gridDim.x / ctas : gridDim.x;
+  constexpr int kUnit = kScaleStageK / kStageK;
+  const int units = (p.kblocks + kUnit - 1) / kUnit;
+  const int kb0 = SPLIT ? units * rank / ctas * kUnit : 0, kb1 = SPLIT ? min(units * (rank + 1) / ctas * kUnit, p.kblocks) : p.kblocks;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) { mbar_init(full0 + 8 * s, 1 + kScaleWarps); mbar_init(empty0 + 8 * s, 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(accf0 + 8 * b, 1); mbar_init(acce0 + 8 * b, kEpi); }
     for (int b = 0; b < kScaleStages; ++b) { mbar_init(ssf0 + 8 * b, 1); mbar_init(sse0 + 8 * b, kScaleWarps); }
+    if constexpr (SPLIT) { mbar_init(partf, (ctas - 1) * kEpi); mbar_init(parte, kEpi); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -202,6 +248,7 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   }
   tc_fence_before();
   __syncthreads();
+  if constexpr (SPLIT) cluster_sync_all();           // the others' barriers exist before anything is sent to them
   tc_fence_after();
   chain_enter();
   const uint32_t tmem_base = *tmem_slot, smem_base = smem_u32(smem), scale_base = smem_base + S * kStage;
@@ -240,13 +287,13 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     // ------------------------------------------------------------------ TMA
     const uint32_t elected = elect_one();
     uint32_t stage = 0, phase = 0, scale_stage = 0, scale_phase = 0, alive = 1;
-    Walk<NT> walk(groups, p.tiles_m);                // of A only the halves of a tile that hold rows are loaded
-    for (int tile = blockIdx.x, step = 0; tile < total; tile += gridDim.x, step = gridDim.x) {
+    Walk<NT> walk(groups, p.tiles_m, first_tile);                // of A only the halves of a tile that hold rows are loaded
+    for (int tile = first_tile, step = 0; tile < total; tile += tile_step, step = tile_step) {
       walk.next(step);
       const int e = __shfl_sync(0xffffffffu, walk.e, 0), col0 = __shfl_sync(0xffffffffu, walk.m, 0) * kM, row0 = __shfl_sync(0xffffffffu, walk.row0, 0);
       const int boxes = __shfl_sync(0xffffffffu, walk.rows > NT / kBoxes ? kBoxes : 1, 0);
-      for (int kb = 0; kb < p.kblocks; ++kb) {
-        if (kb % (kScaleStageK / kStageK) == 0) {
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (kb % kUnit == 0) {
           wait(alive, sse0 + 8 * scale_stage, scale_phase ^ 1, abort_flag, p.status, 7);
           const uint32_t lead = elected & alive;
           const uint32_t sc = scale_base + scale_stage * kScaleStage, bar = ssf0 + 8 * scale_stage;
@@ -271,13 +318,13 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     constexpr uint32_t idesc0 = (1u << 7) | (1u << 10) | (1u << 23) | ((uint32_t)(kM >> 4) << 24);
     const uint32_t elected = elect_one(), low0 = desc_low(smem_base);
     uint32_t stage = 0, phase = 0, it = 0, alive = 1;
-    Walk<NT> walk(groups, p.tiles_m);
-    for (int tile = blockIdx.x, step = 0; tile < total; tile += gridDim.x, step = gridDim.x, ++it) {
+    Walk<NT> walk(groups, p.tiles_m, first_tile);
+    for (int tile = first_tile, step = 0; tile < total; tile += tile_step, step = tile_step, ++it) {
       walk.next(step);
       const uint32_t idesc = __shfl_sync(0xffffffffu, idesc0 | ((uint32_t)(walk.rows + 31) / 32 << 19), 0);
       const uint32_t buf = it & 1, d = buf * NT;
       wait(alive, acce0 + 8 * buf, ((it >> 1) & 1) ^ 1, abort_flag, p.status, 2);
-      for (int kb = 0; kb < p.kblocks; ++kb) {
+      for (int kb = kb0; kb < kb1; ++kb) {
         wait(alive, full0 + 8 * stage, phase, abort_flag, p.status, 4);
         tc_fence_after();
         const uint32_t lead = elected & alive;
@@ -287,7 +334,7 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         for (int i = 0; i < 4; ++i) {
           const uint32_t half = 2 * (i & 1);
           tc_mma_mx_if(blocks > 2 * i ? lead : 0u, d, blow + 2 * i, alow + 2 * i, idesc | (half << 4) | (half << 29), scales + 4 * (i >> 1),
-                       scales + 8 + kColsA * (i >> 1), (kb | i) != 0);
+                       scales + 8 + kColsA * (i >> 1), (kb - kb0 | i) != 0);
         }
         tc_commit_if(lead, empty0 + 8 * stage);
         if (++stage == S) { stage = 0; phase ^= 1; }
@@ -299,9 +346,9 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     constexpr int kRows = NT / 32;                   // of A, a lane's share of a tile; four of B
     uint32_t scale_stage = 0, scale_phase = 0, stage = 0, phase = 0;
-    for (int tile = blockIdx.x; tile < total && !gave_up; tile += gridDim.x) {
-      for (int kb = 0; kb < p.kblocks; ++kb) {
-        const int part = kb % (kScaleStageK / kStageK);
+    for (int tile = first_tile; tile < total && !gave_up; tile += tile_step) {
+      for (int kb = kb0; kb < kb1; ++kb) {
+        const int part = kb % kUnit;
         if (part == 0 && !warp_wait(ssf0 + 8 * scale_stage, scale_phase, abort_flag, p.status, 8, lane)) { gave_up = true; break; }
         // a row's eight bytes of this stage; the TMA unit's 32-byte swizzle exchanges the 16-byte halves of every other four rows
         const uint32_t from = scale_base + scale_stage * kScaleStage + lane * kScaleRow + (((part >> 1) ^ ((lane >> 2) & 1)) << 4) + 8 * (part & 1);
@@ -321,7 +368,7 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 #pragma unroll
           for (int i = 0; i < kColsA; ++i) { v[8 + i] &= first; v[8 + kColsA + i] &= second; }
         }
-        if (part == kScaleStageK / kStageK - 1 || kb + 1 == p.kblocks) {     // all of these scales are in registers
+        if (part == kUnit - 1 || kb + 1 == kb1) {     // all of these scales are in registers
           __syncwarp();
           if (lane == 0) mbar_arrive(sse0 + 8 * scale_stage);
           if (++scale_stage == kScaleStages) { scale_stage = 0; scale_phase ^= 1; }
@@ -342,8 +389,8 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     // ------------------------------------------------------------------ epilogue
     const int q = warp & 3, first = kChunk * ((warp - 2) >> 2);      // chunks of rows in turn with the quarter's other warps
     int it = 0;
-    Walk<NT> walk(groups, p.tiles_m);
-    for (int step = 0; walk.next(step); step = gridDim.x, ++it) {
+    Walk<NT> walk(groups, p.tiles_m, first_tile);
+    for (int step = 0; walk.next(step); step = tile_step, ++it) {
       const int buf = it & 1; const uint32_t use = (uint32_t)(it >> 1);
       const int col = walk.m * kM + q * 32 + lane, rows = walk.rows;
       const bool in = col < p.N;
@@ -355,12 +402,45 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       if (!warp_wait(accf0 + 8 * buf, use & 1, abort_flag, p.status, 6, lane)) { gave_up = true; break; }
       tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + buf * NT;
+      // a chunk of a part: this warp's 32 columns times kChunk rows, four values of a lane after those of the others
+      const uint32_t parts = scale_base + kScaleStages * kScaleStage + q * (32 * kChunk * 4) + lane * 16;
+      constexpr uint32_t kPart = kM * NT * 4, kChunkBytes = kM * kChunk * 4;
+      if constexpr (SPLIT) {
+        if (rank != 0) {
+          if (!cluster_wait(parte, (it & 1) ^ 1, abort_flag, p.status, 10, lane)) { gave_up = true; break; }
+          const uint32_t to = map_to_cta(parts + (rank - 1) * kPart, 0);
+#pragma unroll 1
+          for (int c = first; c < rows; c += kChunk * (kEpi / 4)) {
+            uint32_t r[kChunk]; tc_ld16(taddr + c, r);
+#pragma unroll
+            for (int j = 0; j < kChunk; j += 4) st_cluster4(to + c / kChunk * kChunkBytes + j * 128, reinterpret_cast<const float*>(r) + j);
+          }
+          asm volatile("fence.acq_rel.cluster;" ::: "memory");
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) { mbar_arrive_cluster(map_to_cta(partf, 0)); mbar_arrive(acce0 + 8 * buf); }
+          continue;
+        }
+        if (!cluster_wait(partf, it & 1, abort_flag, p.status, 11, lane)) { gave_up = true; break; }
+      }
 #pragma unroll 1
       for (int c = first; c < rows; c += kChunk * (kEpi / 4)) {     // uniform across the warp
         uint32_t r[kChunk]; tc_ld16(taddr + c, r);
         float v[kChunk];
 #pragma unroll
-        for (int j = 0; j < kChunk; ++j) v[j] = __uint_as_float(r[j]) + bias;
+        for (int j = 0; j < kChunk; ++j) v[j] = __uint_as_float(r[j]);
+        if constexpr (SPLIT) {
+          for (int other = 1; other < ctas; ++other)
+#pragma unroll
+            for (int j = 0; j < kChunk; j += 4) {
+              float4 o;
+              asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(o.x), "=f"(o.y), "=f"(o.z), "=f"(o.w)
+                           : "r"(parts + (other - 1) * kPart + c / kChunk * kChunkBytes + j * 128) : "memory");
+              v[j] += o.x; v[j + 1] += o.y; v[j + 2] += o.z; v[j + 3] += o.w;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) v[j] += bias;
         if (p.act == EC_MX_GELU_ERF) {
 #pragma unroll
           for (int j = 0; j < kChunk; j += 2) gelu_erf2(v[j], v[j + 1]);
@@ -423,6 +503,9 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(acce0 + 8 * buf);
+      if constexpr (SPLIT) {                         // the parts have been read
+        if (lane == 0) for (int other = 1; other < ctas; ++other) mbar_arrive_cluster(map_to_cta(parte, other));
+      }
     }
   }
 
@@ -433,6 +516,7 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   __syncwarp();
   tc_fence_before();
   __syncthreads();
+  if constexpr (SPLIT) cluster_sync_all();           // nobody writes to or arrives at a CTA that has gone
   if (warp == 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kTmemCols) : "memory");
@@ -450,7 +534,10 @@ bool byte_map(CUtensorMap* tm, const void* base, int dims, int64_t inner, int64_
              swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int NT, int OUT>
+// No more row tiles than these: every expert may add one that is not full
+int64_t most_tiles(const MxGemmArgs& g, int nt) { return (g.rows - 1) / nt + (g.E < g.rows ? g.E : g.rows); }
+
+template <int NT, int OUT, bool SPLIT>
 cudaError_t launch_one(const MxGemmArgs& g, MxParams p, int sms, cudaStream_t st) {
   CUtensorMap ta, tb, tas, tbs;
   const int64_t inner = 16 * (int64_t)p.blocks, pitch = 16 * (int64_t)((g.K + 511) / 512);
@@ -458,15 +545,29 @@ cudaError_t launch_one(const MxGemmArgs& g, MxParams p, int sms, cudaStream_t st
       !byte_map(&tb, g.B, 3, inner, g.N, g.E, kRowBytes, kM, CU_TENSOR_MAP_SWIZZLE_128B) ||
       !byte_map(&tas, g.A_scales, 2, pitch, g.rows, 1, kScaleRow, NT, CU_TENSOR_MAP_SWIZZLE_32B) ||
       !byte_map(&tbs, g.B_scales, 3, pitch, g.N, g.E, kScaleRow, kM, CU_TENSOR_MAP_SWIZZLE_32B)) return cudaErrorInvalidValue;
-  constexpr int smem = stages_of(NT) * (kBBytes + NT * kRowBytes) + kScaleStages * scale_stage_bytes(NT) + 1024 + (2 * stages_of(NT) + 5 + 2 * kScaleStages) * 8 +
+  constexpr int S = stages_of(NT, SPLIT);
+  constexpr int smem = S * (kBBytes + NT * kRowBytes) + kScaleStages * scale_stage_bytes(NT) + parts_bytes(NT, SPLIT) + 1024 + (2 * S + 7 + 2 * kScaleStages) * 8 +
                        (int)sizeof(Groups);
   static_assert(smem <= 227 * 1024, "shared memory");
-  auto kern = gemm_mx_kernel<NT, OUT>;
+  auto kern = gemm_mx_kernel<NT, OUT, SPLIT>;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  // no more CTAs than there can be tiles: every expert may add one that is not full
-  const int64_t most = ((g.rows + NT - 1) / NT + (g.E < g.rows ? g.E : g.rows)) * p.tiles_m;
-  return launch_chained(kern, dim3((unsigned)(most < sms ? most : sms)), dim3(kThreads), smem, st, ta, tb, tas, tbs, p);
+  const int64_t most = most_tiles(g, NT) * p.tiles_m, at_once = sms / p.split;
+  return launch_chained_cluster(p.split, kern, dim3((unsigned)((most < at_once ? most : at_once) * p.split)), dim3(kThreads), smem, st, ta, tb, tas, tbs, p);
+}
+// CTAs to a tile: more than one where all tiles then run at once and the contraction is long enough to pay for the joining, about 1 us (one CTA,
+// two, four: two experts' rows, 16384 x 4096, 28.4, 20.5 and, not all at once, 30.0 us; one expert's 28.0, 18.9, 15.4; two of 8192 x 2048
+// 16.1, 12.8, 12.0; two of 2048 x 2048 7.0, 8.0).  Where tiles take several rounds each round joins anew (eight experts, 4096 x 16384: 52 and 70 us).
+int pick_split(const MxGemmArgs& g, const MxParams& p, int nt, int sms) {
+  const int64_t tiles = most_tiles(g, nt) * p.tiles_m;
+  const int units = (p.kblocks + kScaleStageK / kStageK - 1) / (kScaleStageK / kStageK);
+  if (most_split(nt) >= 4 && units >= 8 && tiles * 4 <= sms * 7 / 8) return 4;           // clusters of four do not use every SM
+  return units >= 6 && tiles * 2 <= sms ? 2 : 1;
+}
+template <int NT, int OUT>
+cudaError_t launch_narrow(const MxGemmArgs& g, MxParams p, int sms, cudaStream_t st) {
+  p.split = pick_split(g, p, NT, sms);
+  return p.split > 1 ? launch_one<NT, OUT, true>(g, p, sms, st) : launch_one<NT, OUT, false>(g, p, sms, st);
 }
 template <int OUT>
 cudaError_t launch_out(const MxGemmArgs& g, const MxParams& p, int sms, cudaStream_t st) {
@@ -475,9 +576,9 @@ cudaError_t launch_out(const MxGemmArgs& g, const MxParams& p, int sms, cudaStre
   // choices spread by exp(normal / 2), us for 64, 128, 192: a mean of 32 rows 425, 418, 459; 64 rows 543, 469, 503; 128 rows 839, 619, 598;
   // 256 rows 1510, 964, 843; 512 rows 2921, 1623, 1377; sixteen rows, 1024 x 1024: 15.5, 17.3, 19.2.
   const int64_t mean = g.rows / g.E;
-  if (mean <= 2) return launch_one<32, OUT>(g, p, sms, st);        // eight rows of one token each: 64 us, with tiles of 64 rows 72 (more of the weights on their way)
-  if (mean <= 20) return launch_one<64, OUT>(g, p, sms, st);
-  return mean <= 90 ? launch_one<128, OUT>(g, p, sms, st) : launch_one<192, OUT>(g, p, sms, st);
+  if (mean <= 2) return launch_narrow<32, OUT>(g, p, sms, st);     // eight rows of one token each: 64 us, with tiles of 64 rows 72 (more of the weights on their way)
+  if (mean <= 20) return launch_narrow<64, OUT>(g, p, sms, st);
+  return mean <= 90 ? launch_one<128, OUT, false>(g, p, sms, st) : launch_one<192, OUT, false>(g, p, sms, st);
 }
 
 }  // namespace
@@ -493,7 +594,7 @@ cudaError_t launch_gemm_mx(const MxGemmArgs& g, cudaStream_t st) {
   p.blocks = (g.K + 31) / 32; p.kblocks = (p.blocks + 7) / 8; p.act = g.act; p.offsets = g.offsets;
   p.bias = g.bias; p.bias_f32 = g.bias_dtype == EC_F32; p.c = g.C; p.c_scales = g.C_scales;
   p.c_pitch = 16 * (int64_t)((g.N + 31) / 32); p.c_scale_pitch = 16 * (int64_t)((g.N + 511) / 512);
-  p.status = g.status;
+  p.status = g.status; p.split = 1;
   switch (g.out) {
     case EC_MX_OUT_F32: return launch_out<OUT_F32>(g, p, sms, st);
     case EC_MX_OUT_BF16: return launch_out<OUT_BF16>(g, p, sms, st);

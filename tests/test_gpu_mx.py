@@ -150,7 +150,7 @@ def test_product(rows, N, K, E, kind, dtype):
     assert (_np(out)[np.isnan(z)] == 7.0).all()           # rows of no expert: as they were
 
 
-@pytest.mark.parametrize("rows,N,K,E", [(3, 128, 4096, 2), (40, 136, 4096, 1), (90, 256, 2048, 1), (600, 384, 4096, 2)])
+@pytest.mark.parametrize("rows,N,K,E", [(3, 128, 4096, 2), (40, 136, 4096, 1), (90, 256, 2048, 1), (600, 384, 4096, 2), (2, 264, 4096, 8), (17, 72, 3080, 4), (1, 1000, 1096, 1)])
 def test_sums_that_fp32_holds_are_exact(rows, N, K, E):
     """Scales of 1/2 to 2: every product is a multiple of 2^-4 below 144, a sum of 4096 below 2^20 in steps of 2^-4: 24 bits, so any order of
     exact additions gives the same value."""
@@ -158,6 +158,7 @@ def test_sums_that_fp32_holds_are_exact(rows, N, K, E):
     A, W = B.alloc_mx((rows, K)), B.alloc_mx((E, N, K))
     for q in (A, W):
         q.codes.copy_(torch.randint(0, 256, q.codes.shape, generator=g, dtype=torch.uint8))
+        q.codes[..., K // 2:] = 0                         # what the format wants behind the last column
         q.scales.copy_(torch.randint(126, 129, q.scales.shape, generator=g, dtype=torch.uint8))
     offsets = _groups(rows, E, "even", 0)
     out = B.ec_mx_expert_gemm(A, W, torch.from_numpy(offsets).int().cuda(), dtype=F32)
@@ -334,6 +335,27 @@ def test_expert_choice_slots_through_the_product():
     want = B.ec_expert_gemm(cfg, B.EC_GEMM_XW1, *values)
     size = np.abs(_np(values[0])) @ np.abs(_np(values[1]))
     assert (np.abs(_np(got) - _np(want)) <= 2 * (d + 2) * 2.0 ** -23 * size + 2 * R.HALF_STEP[BF16] * np.abs(_np(want)) + 1e-30).all()
+
+
+@pytest.mark.parametrize("rows,E", [(1, 1), (2, 8), (5, 2), (20, 1), (37, 4), (3, 64)])
+@pytest.mark.parametrize("N,K", [(8, 1032), (136, 2048), (264, 5000), (1096, 8200)])
+def test_few_rows_along_a_long_contraction(rows, E, N, K):
+    """Few tiles: several CTAs share each, at any length of the contraction, also one that their stretches do not divide.  Every result type."""
+    A, W, a, w = _case(rows, N, K, E, rows + N)
+    offsets = _groups(rows, E, "any", 3)
+    off = torch.from_numpy(offsets).int().cuda()
+    bias = torch.randn(E, N, generator=torch.Generator().manual_seed(1)).cuda()
+    z, size = M.product(a, w, offsets, _np(bias))
+    ws = torch.empty(B.EC_MX_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+    full = B.ec_mx_expert_gemm(A, W, off, bias=bias, act="tanh", dtype=F32, ws=ws)
+    assert B.ec_read_status(ws) == B.EC_OK
+    M.check_product(_np(full), z, size, K, F32, "tanh")
+    for _ in range(20):                                   # the order of the sums does not depend on the CTAs' timing
+        assert torch.equal(B.ec_mx_expert_gemm(A, W, off, bias=bias, act="tanh", dtype=F32), full)
+    assert torch.equal(B.ec_mx_expert_gemm(A, W, off, bias=bias, act="tanh", dtype=BF16), full.to(BF16))
+    q = B.ec_mx_expert_gemm(A, W, off, bias=bias, act="tanh", out=B.alloc_mx((rows, N)))
+    codes, scales = M.encode(_np(full))
+    assert np.array_equal(_np(q.codes), codes) and np.array_equal(_np(q.scales)[:, :-(-N // 32)], scales[:, :-(-N // 32)])
 
 
 def test_weights_beyond_the_range_of_32_bit_offsets():
