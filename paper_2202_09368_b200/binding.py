@@ -373,12 +373,13 @@ def ec_combine_backward(cfg, dX_out, Y, weights, place, dY=None, dweights=None):
 
 # ---- products on 4-bit operands ------------------------------------------------------------------------------------------------
 
-@dataclass
 class Mx:
-    """A matrix (or several: leading axes) in the 4-bit microscaled format."""
-    codes: torch.Tensor        # [..., rows, code pitch] uint8
-    scales: torch.Tensor       # [..., rows, scale pitch] uint8
-    cols: int                  # columns: the contraction
+    """A matrix (or several: leading axes) in the 4-bit microscaled format: codes [..., rows, code pitch] and scales [..., rows, scale
+    pitch], both uint8, of `cols` columns (the contraction)."""
+    __slots__ = ("codes", "scales", "cols")
+
+    def __init__(self, codes, scales, cols):
+        self.codes, self.scales, self.cols = codes, scales, cols
 
 
 def _mx_pitches(cols):

@@ -99,8 +99,8 @@ ec_status ec_mx_dispatch(const ec_sort_config* c, const void* X, const int32_t* 
   return EC_OK;
 }
 
-ec_status ec_mx_expert_gemm(const ec_mx_gemm_config* c, const uint8_t* A, const uint8_t* A_scales, const int32_t* offsets, const uint8_t* B,
-                            const uint8_t* B_scales, const void* bias, void* C, uint8_t* C_scales, void* ws, size_t ws_bytes, void* stream) {
+static ec_status mx_expert_gemm(const ec_mx_gemm_config* c, const uint8_t* A, const uint8_t* A_scales, const int32_t* offsets, const uint8_t* B,
+                                const uint8_t* B_scales, const void* bias, void* C, uint8_t* C_scales, void* ws, size_t ws_bytes, int silent, void* stream) {
   if (!c || c->rows < 0 || c->N < 1 || c->K < 1 || c->E < 1) return EC_ERR_INVALID_ARG;
   if (c->out < EC_MX_OUT_F32 || c->out > EC_MX_OUT_MX || c->act < EC_MX_NONE || c->act > EC_MX_GELU_TANH) return EC_ERR_INVALID_ARG;
   if (c->bias_dtype != EC_F32 && c->bias_dtype != EC_BF16) return EC_ERR_INVALID_ARG;
@@ -112,7 +112,20 @@ ec_status ec_mx_expert_gemm(const ec_mx_gemm_config* c, const uint8_t* A, const 
   if (c->rows == 0) return EC_OK;
   if (bad_pointers(A, A_scales, offsets, B, B_scales, C) || (bias != nullptr && misaligned(bias, 16))) return EC_ERR_INVALID_ARG;
   if (c->out == EC_MX_OUT_MX ? bad_pointers(C_scales) : C_scales != nullptr) return EC_ERR_INVALID_ARG;
-  MxGemmArgs g{c->rows, c->N, c->K, c->E, c->out, c->act, A, A_scales, offsets, B, B_scales, bias, c->bias_dtype, C, C_scales, (int*)ws};
+  MxGemmArgs g{c->rows, c->N, c->K, c->E, c->out, c->act, A, A_scales, offsets, B, B_scales, bias, c->bias_dtype, C, C_scales, (int*)ws, silent};
   EC_CUDA(launch_gemm_mx(g, (cudaStream_t)stream));
   return EC_OK;
 }
+
+ec_status ec_mx_expert_gemm(const ec_mx_gemm_config* c, const uint8_t* A, const uint8_t* A_scales, const int32_t* offsets, const uint8_t* B,
+                            const uint8_t* B_scales, const void* bias, void* C, uint8_t* C_scales, void* ws, size_t ws_bytes, void* stream) {
+  return mx_expert_gemm(c, A, A_scales, offsets, B, B_scales, bias, C, C_scales, ws, ws_bytes, 0, stream);
+}
+
+#ifdef EC_DEBUG
+// ec_mx_expert_gemm in which the first CTA loads nothing, so that its waits run out, and those of its cluster.
+extern "C" ec_status ec_debug_mx_wait(const ec_mx_gemm_config* c, const uint8_t* A, const uint8_t* A_scales, const int32_t* offsets, const uint8_t* B,
+                                      const uint8_t* B_scales, const void* bias, void* C, uint8_t* C_scales, void* ws, size_t ws_bytes, void* stream) {
+  return mx_expert_gemm(c, A, A_scales, offsets, B, B_scales, bias, C, C_scales, ws, ws_bytes, 1, stream);
+}
+#endif

@@ -67,6 +67,9 @@ struct MxParams {
   const void* bias; int bias_f32;
   void* c; uint8_t* c_scales; int64_t c_pitch, c_scale_pitch;     // c_pitch in bytes
   int* status;
+#ifdef EC_DEBUG
+  int silent;                                        // see ec_debug_mx_wait
+#endif
 };
 
 enum { OUT_F32 = 0, OUT_BF16 = 1, OUT_MX = 2 };
@@ -287,8 +290,13 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     // ------------------------------------------------------------------ TMA
     const uint32_t elected = elect_one();
     uint32_t stage = 0, phase = 0, scale_stage = 0, scale_phase = 0, alive = 1;
-    Walk<NT> walk(groups, p.tiles_m, first_tile);                // of A only the halves of a tile that hold rows are loaded
-    for (int tile = first_tile, step = 0; tile < total; tile += tile_step, step = tile_step) {
+#ifdef EC_DEBUG
+    const int last_tile = p.silent && blockIdx.x == 0 ? 0 : total;
+#else
+    const int last_tile = total;
+#endif
+    Walk<NT> walk(groups, p.tiles_m, first_tile);    // of A only the halves of a tile that hold rows are loaded
+    for (int tile = first_tile, step = 0; tile < last_tile; tile += tile_step, step = tile_step) {
       walk.next(step);
       const int e = __shfl_sync(0xffffffffu, walk.e, 0), col0 = __shfl_sync(0xffffffffu, walk.m, 0) * kM, row0 = __shfl_sync(0xffffffffu, walk.row0, 0);
       const int boxes = __shfl_sync(0xffffffffu, walk.rows > NT / kBoxes ? kBoxes : 1, 0);
@@ -595,6 +603,9 @@ cudaError_t launch_gemm_mx(const MxGemmArgs& g, cudaStream_t st) {
   p.bias = g.bias; p.bias_f32 = g.bias_dtype == EC_F32; p.c = g.C; p.c_scales = g.C_scales;
   p.c_pitch = 16 * (int64_t)((g.N + 31) / 32); p.c_scale_pitch = 16 * (int64_t)((g.N + 511) / 512);
   p.status = g.status; p.split = 1;
+#ifdef EC_DEBUG
+  p.silent = g.silent;
+#endif
   switch (g.out) {
     case EC_MX_OUT_F32: return launch_out<OUT_F32>(g, p, sms, st);
     case EC_MX_OUT_BF16: return launch_out<OUT_BF16>(g, p, sms, st);

@@ -194,6 +194,7 @@ struct MxGemmArgs {
   const void* A; const uint8_t* A_scales; const int32_t* offsets; const void* B; const uint8_t* B_scales;
   const void* bias; int bias_dtype;                // [E, N] or null
   void* C; uint8_t* C_scales; int* status;
+  int silent;                                      // debug build: the first CTA loads nothing, see ec_debug_mx_wait
 };
 cudaError_t launch_gemm_mx(const MxGemmArgs& g, cudaStream_t st);
 

@@ -1,0 +1,35 @@
+"""The 4-bit products in the debug build: the same bits as the normal one, and waits that run out are reported, not waited for."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2202_09368_b200 import binding as B
+
+from test_gpu_debug_build import D  # noqa: F401  (the fixture: a second binding, of the debug library)
+
+pytestmark = pytest.mark.gpu
+
+
+def _operands(M, rows, N, K, E):
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    A = M.ec_mx_quantize(torch.empty(rows, K, device="cuda").normal_(generator=g))
+    W = M.ec_mx_quantize(torch.empty(E, N, K, device="cuda").normal_(generator=g))
+    return A, W, torch.arange(E + 1, dtype=torch.int32, device="cuda") * (rows // E)
+
+
+@pytest.mark.parametrize("rows,N,K,E", [(1, 128, 8192, 1), (30, 264, 6144, 2), (64, 256, 512, 2), (300, 1000, 1000, 2), (900, 384, 512, 2)])
+def test_a_product_whose_loads_never_come(D, rows, N, K, E):
+    """One CTA loads nothing: the call ends, with the status of a wait that ran out, and the next one on the same workspace is as ever."""
+    A, W, offsets = _operands(D, rows, N, K, E)
+    ws = torch.empty(D.EC_MX_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+    want = D.ec_mx_expert_gemm(A, W, offsets, ws=ws)
+    assert D.ec_read_status(ws) == D.EC_OK and torch.equal(want, B.ec_mx_expert_gemm(A, W, offsets))
+    cfg = D.ec_mx_gemm_config(rows, N, K, E, D.EC_MX_OUT_BF16, 0, 0)
+    call = D.lib().ec_debug_mx_wait
+    call.argtypes = [ctypes.POINTER(D.ec_mx_gemm_config)] + [ctypes.c_void_p] * 9 + [ctypes.c_size_t, ctypes.c_void_p]
+    out = torch.zeros_like(want)
+    assert call(ctypes.byref(cfg), A.codes.data_ptr(), A.scales.data_ptr(), offsets.data_ptr(), W.codes.data_ptr(), W.scales.data_ptr(), None,
+                out.data_ptr(), None, ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream) == D.EC_OK
+    assert D.ec_read_status(ws) == D.EC_ERR_TIMEOUT
+    assert torch.equal(D.ec_mx_expert_gemm(A, W, offsets, ws=ws), want) and D.ec_read_status(ws) == D.EC_OK
