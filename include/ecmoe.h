@@ -316,7 +316,7 @@ typedef struct {
 size_t ec_sort_workspace_bytes(const ec_sort_config* cfg);
 
 /* The plan: offsets, order and place of `choice`.  Counting and ranking only, no atomics on global memory: the result is unique.
- * One launch up to 16384 choices, two beyond. */
+ * One launch up to 24576 choices, two beyond. */
 ec_status ec_sort_tokens(const ec_sort_config* cfg, const int32_t* choice, int32_t* offsets, int32_t* order, int32_t* place,
                          void* ws, size_t ws_bytes, void* cuda_stream);
 

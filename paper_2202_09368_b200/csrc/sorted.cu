@@ -10,124 +10,190 @@ namespace {
 
 // ---- the plan ----------------------------------------------------------------------------------------------
 // A counting sort.  The flat choices are cut into one contiguous piece per CTA and those into one per warp; a choice's row is
-//   offsets[e] + (choices of e in earlier CTAs) + (in earlier warps of this CTA) + (earlier in this warp),
-// all of them plain counts, so the order is the stable one and unique.  A warp counts 32 choices at a time: the lanes with the
-// same expert find each other (match), the lowest adds their number to the warp's own row of counters in shared memory.
-// Up to kOnePiece choices one CTA does it all; beyond, a first launch leaves every CTA's counts and in the second each CTA sums
-// what it needs of them (148 x 256 counters at most, 148 KiB out of L2).
-constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kMaxExperts = 256;
-constexpr int64_t kOnePiece = 4096;
+//   offsets[e] + (choices of e in earlier pieces) + (in earlier warps of this piece) + (earlier in this warp),
+// all of them plain counts, so the order is the stable one and unique.  A warp ranks 32 choices at a time: the lanes with the
+// same expert find each other by one vote per bit of its number (a match instruction takes three times as long), the lowest of them
+// adds their number to the warp's own row of counters in shared memory.
+// Up to kOnePiece choices one CTA does it all, up to kClusterMost the eight of a cluster, which read each other's counts in shared
+// memory; beyond, a first launch leaves each piece's counts and, in `place`, ranks inside the piece, and in a second each CTA sums what it
+// needs of the counts (148 x 256 at most, 148 KiB out of L2) and adds.
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kMaxExperts = 256, kClusterCtas = 8;
+constexpr int64_t kOnePiece = 2048, kClusterMost = 24576;
 constexpr int kMaxPieces = 148;
+constexpr int kHeld = 4;                              // rounds of 32 choices whose ranks a warp keeps in registers
+enum { ONE_CTA, ONE_CLUSTER, TWO_LAUNCHES };
 
 struct SortArgs {
   const int32_t* choice; int32_t* offsets; int32_t* order; int32_t* place; int* counts;   // counts [pieces, E]
   int64_t total, per_cta;                                                                  // flat choices; per_cta a multiple of 1024
-  int E, pieces;
+  int E, bits, pieces;                                                                     // bits: of an expert's number
 };
 
-// counts of one warp's stretch [lo, hi) into mine[0 .. E)
-__device__ __forceinline__ void count_stretch(const int32_t* choice, int64_t lo, int64_t hi, int E, int* mine, int lane) {
-  constexpr int U = 8;                                  // choices on their way per lane
-  for (int64_t i = lo; i < hi; i += 32 * U) {
-    int e[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) { const int64_t at = i + 32 * u + lane; e[u] = at < hi ? __ldg(choice + at) : -1; }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const bool in = (unsigned)e[u] < (unsigned)E;
-      const unsigned peers = __match_any_sync(0xffffffffu, in ? e[u] : -1);
-      if (in && (peers & ((1u << lane) - 1)) == 0) mine[e[u]] += __popc(peers);
-      __syncwarp();
-    }
+// One round: the number of earlier choices of the same expert in the warp's stretch, counters moved on.
+__device__ __forceinline__ int rank_round(int e, bool in, int bits, int* mine, int lane) {
+  unsigned peers = __ballot_sync(0xffffffffu, in);
+  for (int b = 0; b < bits; ++b) {
+    const bool one = (e >> b) & 1;
+    const unsigned with = __ballot_sync(0xffffffffu, one);
+    peers &= one ? with : ~with;
   }
-}
-
-__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs a) {
-  __shared__ int counters[kSortWarps][kMaxExperts];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int e = lane; e < a.E; e += 32) counters[warp][e] = 0;
+  const int before = __popc(peers & ((1u << lane) - 1));
+  const int at = in ? mine[e] + before : -1;
   __syncwarp();
-  chain_enter();
-  const int32_t* choice = after_enter(a.choice);
-  const int64_t per_warp = a.per_cta / kSortWarps, lo = blockIdx.x * a.per_cta + warp * per_warp;
-  count_stretch(choice, lo, min(lo + per_warp, a.total), a.E, counters[warp], lane);
-  __syncthreads();
-  if (threadIdx.x < a.E) {
-    int sum = 0;
-#pragma unroll
-    for (int w = 0; w < kSortWarps; ++w) sum += counters[w][threadIdx.x];
-    a.counts[(int64_t)blockIdx.x * a.E + threadIdx.x] = sum;
-  }
+  if (in && before == 0) mine[e] += __popc(peers);
+  __syncwarp();
+  return at;
 }
 
-template <bool ONE>
-__global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortArgs a) {
+// Exclusive sums of v over the 256 threads with part = 0 (in order of e); every thread of the CTA calls it.
+__device__ __forceinline__ int scan_experts(int v, int part, int warp, int lane, int* warp_sum) {
+  int incl = v;
+#pragma unroll
+  for (int o = 1; o < 32; o *= 2) { const int u = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += u; }
+  if (part == 0 && lane == 31) warp_sum[warp] = incl;
+  __syncthreads();
+  int first = incl - v;
+  if (part == 0) for (int w = 0; w < warp; ++w) first += warp_sum[w];
+  return first;
+}
+
+template <int HOW>
+__global__ void __launch_bounds__(kSortThreads) sort_rank_kernel(const SortArgs a) {
   __shared__ int counters[kSortWarps][kMaxExperts];
-  __shared__ int before[4][kMaxExperts], all[4][kMaxExperts];            // of the pieces, in four parts
-  __shared__ int start[kMaxExperts], warp_sum[kMaxExperts / 32];
+  __shared__ int parts[4][kMaxExperts], earlier[4][kMaxExperts];         // per expert: of eight warps each; of the cluster's pieces in four parts
+  __shared__ int own[kMaxExperts], start[kMaxExperts], warp_sum[kMaxExperts / 32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, E = a.E;
   for (int e = lane; e < E; e += 32) counters[warp][e] = 0;
   __syncwarp();
   chain_enter();
   const int32_t* choice = after_enter(a.choice);
   const int64_t per_warp = a.per_cta / kSortWarps, lo = blockIdx.x * a.per_cta + warp * per_warp, hi = min(lo + per_warp, a.total);
-  count_stretch(choice, lo, hi, E, counters[warp], lane);
-  const int e = threadIdx.x & (kMaxExperts - 1), part = threadIdx.x / kMaxExperts;
-  if constexpr (!ONE) {
-    const int* counts = after_enter((const int*)a.counts);
-    int b = 0, t = 0;
-    if (e < E)
-#pragma unroll 8
-      for (int p = part; p < a.pieces; p += 4) { const int c = __ldg(counts + (int64_t)p * E + e); t += c; if (p < (int)blockIdx.x) b += c; }
-    before[part][e] = b; all[part][e] = t;
-  }
-  __syncthreads();
-  // exclusive sums over the warps per expert, then over the experts
-  int total = 0;
-  if (part == 0) {
-    if (e < E) {
-      int run = 0;
-#pragma unroll
-      for (int w = 0; w < kSortWarps; ++w) { const int c = counters[w][e]; counters[w][e] = run; run += c; }
-      total = ONE ? run : all[0][e] + all[1][e] + all[2][e] + all[3][e];
-    }
-    int incl = total;
-#pragma unroll
-    for (int o = 1; o < 32; o *= 2) { const int v = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += v; }
-    if (lane == 31) warp_sum[warp] = incl;
-    start[e] = incl - total;
-  }
-  __syncthreads();
-  if (part == 0) {
-    int first = start[e];
-    for (int w = 0; w < warp; ++w) first += warp_sum[w];
-    if (blockIdx.x == 0 && e < E) {
-      a.offsets[e] = first;
-      if (e == E - 1) a.offsets[E] = first + total;
-    }
-    start[e] = first + (ONE ? 0 : before[0][e] + before[1][e] + before[2][e] + before[3][e]);
-  }
-  __syncthreads();
   int* mine = counters[warp];
-  for (int i = lane; i < E; i += 32) mine[i] += start[i];
-  __syncwarp();
-  constexpr int U = 8;
-  for (int64_t i = lo; i < hi; i += 32 * U) {
-    int x[U];
+  int held_e[kHeld], held[kHeld];
 #pragma unroll
-    for (int u = 0; u < U; ++u) { const int64_t at = i + 32 * u + lane; x[u] = at < hi ? __ldg(choice + at) : -1; }
+  for (int u = 0; u < kHeld; ++u) { const int64_t at = lo + 32 * u + lane; held_e[u] = at < hi ? __ldg(choice + at) : -1; }
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) if (lo + 32 * u < hi) held[u] = rank_round(held_e[u], (unsigned)held_e[u] < (unsigned)E, a.bits, mine, lane);
+  for (int64_t i = lo + 32 * kHeld; i < hi; i += 32 * kHeld) {           // the ranks of later rounds wait in `place`
+    int e[kHeld];
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) { const int64_t at = i + 32 * u + lane; e[u] = at < hi ? __ldg(choice + at) : -1; }
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) {
+      if (i + 32 * u >= hi) break;
+      const int64_t at = i + 32 * u + lane;
+      const int r = rank_round(e[u], (unsigned)e[u] < (unsigned)E, a.bits, mine, lane);
+      if (at < hi) a.place[at] = r;
+    }
+  }
+  __syncthreads();
+  // per expert, exclusive sums over the warps, eight to a thread
+  const int e = threadIdx.x & (kMaxExperts - 1), part = threadIdx.x / kMaxExperts;
+  int c[8], sum = 0;
+  if (e < E)
+#pragma unroll
+    for (int w = 0; w < 8; ++w) { c[w] = counters[part * 8 + w][e]; sum += c[w]; }
+  parts[part][e] = sum;
+  __syncthreads();
+  int piece = 0, base = 0;                            // of the whole piece; of the parts before
+#pragma unroll
+  for (int q = 0; q < 4; ++q) { piece += parts[q][e]; if (q < part) base += parts[q][e]; }
+  if (HOW == TWO_LAUNCHES && part == 0 && e < E) a.counts[(int64_t)blockIdx.x * E + e] = piece;
+  int first = 0;                                      // part 0: the expert's first row in this piece
+  if constexpr (HOW == ONE_CLUSTER) {
+    if (part == 0) own[e] = piece;
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    int before = 0, all = 0;
+#pragma unroll
+    for (int q = 0; q < kClusterCtas / 4; ++q) {
+      const int p = part + 4 * q;
+      uint32_t there;
+      int n;
+      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(own + e)), "r"(p));
+      asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(n) : "r"(there) : "memory");
+      all += n;
+      if (p < (int)blockIdx.x) before += n;
+    }
+    // nobody leaves while its counts are read: arrived here, waited for at the end
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    earlier[part][e] = before;
+    __syncthreads();                                  // parts has been read
+    parts[part][e] = all;
+    __syncthreads();
+    if (part == 0) { all = parts[0][e] + parts[1][e] + parts[2][e] + parts[3][e]; before = earlier[0][e] + earlier[1][e] + earlier[2][e] + earlier[3][e]; }
+    first = scan_experts(all, part, warp, lane, warp_sum);
+    if (part == 0) {
+      if (blockIdx.x == 0 && e < E) { a.offsets[e] = first; if (e == E - 1) a.offsets[E] = first + all; }
+      start[e] = first + before;
+    }
+  } else if constexpr (HOW == ONE_CTA) {
+    first = scan_experts(piece, part, warp, lane, warp_sum);
+    if (part == 0) {
+      if (e < E) { a.offsets[e] = first; if (e == E - 1) a.offsets[E] = first + piece; }
+      start[e] = first;
+    }
+  } else {
+    if (part == 0) start[e] = 0;
+  }
+  __syncthreads();
+  if (e < E) {
+    base += start[e];
+#pragma unroll
+    for (int w = 0; w < 8; ++w) { counters[part * 8 + w][e] = base; base += c[w]; }
+  }
+  __syncthreads();
+  auto put = [&](int64_t at, int x, int r) {
+    if (at >= hi) return;
+    const int row = r < 0 ? -1 : r + mine[x];
+    a.place[at] = row;
+    if (HOW != TWO_LAUNCHES && row >= 0) a.order[row] = (int)at;
+  };
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) if (lo + 32 * u < hi) put(lo + 32 * u + lane, held_e[u], held[u]);
+  for (int64_t i = lo + 32 * kHeld; i < hi; i += 32 * kHeld) {
+    int x[kHeld], r[kHeld];
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) { const int64_t at = i + 32 * u + lane; if (at < hi) { x[u] = __ldg(choice + at); r[u] = a.place[at]; } }
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) put(i + 32 * u + lane, x[u], r[u]);
+  }
+  if constexpr (HOW == ONE_CLUSTER) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+__global__ void __launch_bounds__(kSortThreads) sort_shift_kernel(const SortArgs a) {
+  __shared__ int before[4][kMaxExperts], all[4][kMaxExperts];            // of the pieces, in four parts
+  __shared__ int start[kMaxExperts], warp_sum[kMaxExperts / 32];
+  chain_enter();
+  const int32_t* choice = after_enter(a.choice);
+  const int* counts = after_enter((const int*)a.counts);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, E = a.E, e = threadIdx.x & (kMaxExperts - 1), part = threadIdx.x / kMaxExperts;
+  int b = 0, t = 0;
+  if (e < E)
+#pragma unroll 16
+    for (int p = part; p < a.pieces; p += 4) { const int c = __ldg(counts + (int64_t)p * E + e); t += c; if (p < (int)blockIdx.x) b += c; }
+  before[part][e] = b; all[part][e] = t;
+  __syncthreads();
+  int total = 0;
+  if (part == 0) { total = all[0][e] + all[1][e] + all[2][e] + all[3][e]; b = before[0][e] + before[1][e] + before[2][e] + before[3][e]; }
+  const int first = scan_experts(total, part, warp, lane, warp_sum);
+  if (part == 0) {
+    if (blockIdx.x == 0 && e < E) { a.offsets[e] = first; if (e == E - 1) a.offsets[E] = first + total; }
+    start[e] = first + b;
+  }
+  __syncthreads();
+  const int64_t lo = blockIdx.x * a.per_cta, hi = min(lo + a.per_cta, a.total);
+  constexpr int U = 4;
+  for (int64_t i = lo + threadIdx.x; i < hi; i += kSortThreads * U) {
+    int x[U], r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) { const int64_t at = i + kSortThreads * u; if (at < hi) { x[u] = __ldg(choice + at); r[u] = a.place[at]; } }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t at = i + 32 * u + lane;
-      const bool in = (unsigned)x[u] < (unsigned)E;
-      const unsigned peers = __match_any_sync(0xffffffffu, in ? x[u] : -1);
-      const int rank = __popc(peers & ((1u << lane) - 1));
-      const int row = in ? mine[x[u]] + rank : -1;
-      __syncwarp();
-      if (in && rank == 0) mine[x[u]] += __popc(peers);
-      __syncwarp();
-      if (at < hi) a.place[at] = row;
-      if (in) a.order[row] = (int)at;
+      const int64_t at = i + kSortThreads * u;
+      if (at >= hi || r[u] < 0) continue;             // without an expert: -1 already
+      const int row = r[u] + start[x[u]];
+      a.place[at] = row;
+      a.order[row] = (int)at;
     }
   }
 }
@@ -392,15 +458,21 @@ cudaError_t backward_of(const void* dX_out, const void* Y, const float* w, const
 size_t sort_scratch_bytes(int E) { return (size_t)kMaxPieces * E * 4; }
 
 cudaError_t launch_sort_tokens(const int32_t* choice, int64_t total, int E, int32_t* offsets, int32_t* order, int32_t* place, void* scratch, cudaStream_t st) {
-  SortArgs a{choice, offsets, order, place, (int*)scratch, total, 0, E, 1};
+  SortArgs a{choice, offsets, order, place, (int*)scratch, total, 0, E, 0, 1};
+  while ((1 << a.bits) < E) ++a.bits;
+  auto cut = [&](int ctas) { a.per_cta = ((total + ctas - 1) / ctas + 1023) / 1024 * 1024; };
   if (total <= kOnePiece) {
-    a.per_cta = (total + 1023) / 1024 * 1024;
-    return launch_chained(sort_place_kernel<true>, dim3(1), dim3(kSortThreads), 0, st, a);
+    cut(1);
+    return launch_chained(sort_rank_kernel<ONE_CTA>, dim3(1), dim3(kSortThreads), 0, st, a);
   }
-  a.per_cta = ((total + kMaxPieces - 1) / kMaxPieces + 1023) / 1024 * 1024;
+  if (total <= kClusterMost) {                        // the last CTAs may have no choices
+    cut(kClusterCtas);
+    return launch_chained_cluster(kClusterCtas, sort_rank_kernel<ONE_CLUSTER>, dim3(kClusterCtas), dim3(kSortThreads), 0, st, a);
+  }
+  cut(kMaxPieces);
   a.pieces = (int)((total + a.per_cta - 1) / a.per_cta);
-  const cudaError_t e = launch_chained(sort_count_kernel, dim3(a.pieces), dim3(kSortThreads), 0, st, a);
-  return e != cudaSuccess ? e : launch_chained(sort_place_kernel<false>, dim3(a.pieces), dim3(kSortThreads), 0, st, a);
+  const cudaError_t e = launch_chained(sort_rank_kernel<TWO_LAUNCHES>, dim3(a.pieces), dim3(kSortThreads), 0, st, a);
+  return e != cudaSuccess ? e : launch_chained(sort_shift_kernel, dim3(a.pieces), dim3(kSortThreads), 0, st, a);
 }
 
 cudaError_t launch_dispatch(const void* X, const int32_t* place, void* X_s, int64_t n, int64_t row_bytes, int K, cudaStream_t st) {

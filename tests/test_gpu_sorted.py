@@ -43,6 +43,7 @@ def _check_plan(got, choice, E):
     (0, 2, 8, "random"), (1, 1, 1, "random"), (1, 2, 64, "distinct"), (1, 32, 256, "distinct"), (2, 3, 5, "holes"), (31, 1, 4, "random"),
     (33, 1, 4, "random"), (255, 4, 256, "holes"), (1000, 3, 10, "holes"), (1024, 1, 64, "random"), (1025, 1, 64, "random"), (777, 5, 7, "one"), (500, 2, 16, "none"),
     (8192, 2, 32, "distinct"), (16384, 1, 64, "random"), (16385, 1, 64, "random"), (6079, 3, 10, "holes"), (16384, 2, 64, "distinct"), (65536, 8, 256, "distinct"),
+    (4096, 1, 16, "random"), (4097, 1, 16, "holes"), (2048, 1, 16, "holes"), (2049, 1, 200, "holes"), (24576, 1, 64, "random"), (24577, 1, 64, "holes"), (2731, 3, 256, "holes"), (5000, 1, 4, "one"), (32768, 2, 128, "holes"), (65537, 1, 64, "random"), (60000, 1, 1, "one"),
     (100003, 7, 33, "holes"), (151552, 1, 256, "random"), (151553, 1, 256, "one"), (540001, 8, 200, "holes"), (30000, 2, 3, "none"),
 ])
 def test_plan(n, K, E, kind):
