@@ -299,20 +299,22 @@ _TYPES = {EC_F32: torch.float32, EC_BF16: torch.bfloat16}
 
 
 def _dense(what, dev, *tensors):
-    """The operands of one of the calls below: dense device tensors of one device, each (tensor, dtype, shape).  The library sees addresses
+    """The operands of one of the calls below: dense tensors of device `dev` (an index), each (tensor, dtype, shape).  The library sees addresses
     only, so what is not like this is refused here.  Returns their addresses."""
     out = []
     for t, dtype, shape in tensors:
-        if t.dtype is not dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
-            raise EcError(EC_ERR_INVALID_ARG, f"{what}: wanted a dense {dtype} tensor {tuple(shape)} on {dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+            raise EcError(EC_ERR_INVALID_ARG, f"{what}: wanted a dense {dtype} tensor {tuple(shape)} on device {dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
         out.append(t.data_ptr())
     return out
 
 
-def _stream_of(what, dev):
-    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
-        raise EcError(EC_ERR_INVALID_ARG, f"{what}: the operands are on {dev}, which is not the current CUDA device")
-    return torch._C._cuda_getCurrentRawStream(dev.index)
+def _device_of(what, t):
+    """The index of t's device, which has to be the current one, and its current stream."""
+    dev = t.get_device()
+    if dev < 0 or dev != torch._C._cuda_getDevice():
+        raise EcError(EC_ERR_INVALID_ARG, f"{what}: the operands are on {t.device}, which is not the current CUDA device")
+    return dev, torch._C._cuda_getCurrentRawStream(dev)
 
 
 @dataclass
@@ -324,8 +326,8 @@ class Sorted:
 
 def ec_sort_tokens(cfg, choice, out: Sorted | None = None, ws=None) -> Sorted:
     """The plan of a dropless token-choice layer: choice [n, per_token] int32 holds each token's experts (outside [0, E): none)."""
-    dev, n, K, E = choice.device, cfg.n, cfg.per_token, cfg.E
-    stream = _stream_of("ec_sort_tokens", dev)
+    dev, stream = _device_of("ec_sort_tokens", choice)
+    n, K, E = cfg.n, cfg.per_token, cfg.E
     if out is None:
         out = Sorted(torch.empty(E + 1, dtype=torch.int32, device=dev), torch.empty(n * K, dtype=torch.int32, device=dev),
                      torch.empty(n, K, dtype=torch.int32, device=dev))
@@ -334,40 +336,40 @@ def ec_sort_tokens(cfg, choice, out: Sorted | None = None, ws=None) -> Sorted:
     i32 = torch.int32
     c, o, r, p, w = _dense("ec_sort_tokens", dev, (choice, i32, (n, K)), (out.offsets, i32, (E + 1,)), (out.order, i32, (n * K,)),
                            (out.place, i32, (n, K)), (ws, torch.uint8, ws.shape))
-    _check(lib().ec_sort_tokens(C.byref(cfg), c, o, r, p, w, ws.numel(), stream), "ec_sort_tokens")
+    _check(lib().ec_sort_tokens(cfg, c, o, r, p, w, ws.numel(), stream), "ec_sort_tokens")
     return out
 
 
 def ec_dispatch(cfg, X, place, X_s=None):
     """X_s[place[t, j], :] = X[t, :]; rows of X_s that no choice holds are left as they were.  Gradient: ec_combine(cfg, dX_s, None, place)."""
-    dev, n, K, d, dt = X.device, cfg.n, cfg.per_token, cfg.d_model, _TYPES[cfg.dtype]
-    stream = _stream_of("ec_dispatch", dev)
+    dev, stream = _device_of("ec_dispatch", X)
+    n, K, d, dt = cfg.n, cfg.per_token, cfg.d_model, _TYPES[cfg.dtype]
     X_s = torch.empty(n * K, d, dtype=dt, device=dev) if X_s is None else X_s
     x, p, s = _dense("ec_dispatch", dev, (X, dt, (n, d)), (place, torch.int32, (n, K)), (X_s, dt, (n * K, d)))
-    _check(lib().ec_dispatch(C.byref(cfg), x, p, s, stream), "ec_dispatch")
+    _check(lib().ec_dispatch(cfg, x, p, s, stream), "ec_dispatch")
     return X_s
 
 
 def ec_combine(cfg, Y, weights, place, X_out=None):
     """X_out[t, :] = sum_j weights[t, j] * Y[place[t, j], :]; weights None: all ones."""
-    dev, n, K, d, dt = Y.device, cfg.n, cfg.per_token, cfg.d_model, _TYPES[cfg.dtype]
-    stream = _stream_of("ec_combine", dev)
+    dev, stream = _device_of("ec_combine", Y)
+    n, K, d, dt = cfg.n, cfg.per_token, cfg.d_model, _TYPES[cfg.dtype]
     X_out = torch.empty(n, d, dtype=dt, device=dev) if X_out is None else X_out
     y, p, x = _dense("ec_combine", dev, (Y, _TYPES[cfg.y_dtype], (n * K, d)), (place, torch.int32, (n, K)), (X_out, dt, (n, d)))
     w = None if weights is None else _dense("ec_combine", dev, (weights, torch.float32, (n, K)))[0]
-    _check(lib().ec_combine(C.byref(cfg), y, w, p, x, stream), "ec_combine")
+    _check(lib().ec_combine(cfg, y, w, p, x, stream), "ec_combine")
     return X_out
 
 
 def ec_combine_backward(cfg, dX_out, Y, weights, place, dY=None, dweights=None):
     """Gradients of ec_combine: (dY [n * per_token, d], rows that no choice holds left as they were; dweights [n, per_token] fp32)."""
-    dev, n, K, d, ty = Y.device, cfg.n, cfg.per_token, cfg.d_model, _TYPES[cfg.y_dtype]
-    stream = _stream_of("ec_combine_backward", dev)
+    dev, stream = _device_of("ec_combine_backward", Y)
+    n, K, d, ty = cfg.n, cfg.per_token, cfg.d_model, _TYPES[cfg.y_dtype]
     dY = torch.empty(n * K, d, dtype=ty, device=dev) if dY is None else dY
     dweights = torch.empty(n, K, dtype=torch.float32, device=dev) if dweights is None else dweights
     g, y, w, p, dy, dw = _dense("ec_combine_backward", dev, (dX_out, _TYPES[cfg.dtype], (n, d)), (Y, ty, (n * K, d)), (weights, torch.float32, (n, K)),
                                 (place, torch.int32, (n, K)), (dY, ty, (n * K, d)), (dweights, torch.float32, (n, K)))
-    _check(lib().ec_combine_backward(C.byref(cfg), g, y, w, p, dy, dw, stream), "ec_combine_backward")
+    _check(lib().ec_combine_backward(cfg, g, y, w, p, dy, dw, stream), "ec_combine_backward")
     return dY, dweights
 
 
@@ -408,8 +410,8 @@ def _dtype_code(what, dtype):
 
 def ec_mx_quantize(X, transposed=False, out: Mx | None = None) -> Mx:
     """X [..., rows, cols], or with `transposed` [..., cols, rows], in the 4-bit format with blocks along cols."""
-    dev, dt = X.device, _dtype_code("ec_mx_quantize", X.dtype)
-    stream = _stream_of("ec_mx_quantize", dev)
+    dt = _dtype_code("ec_mx_quantize", X.dtype)
+    dev, stream = _device_of("ec_mx_quantize", X)
     if X.dim() < 2:
         raise EcError(EC_ERR_INVALID_ARG, "ec_mx_quantize: wanted a matrix")
     lead, (rows, cols) = tuple(X.shape[:-2]), (X.shape[:-3:-1] if transposed else X.shape[-2:])
@@ -427,8 +429,8 @@ def ec_mx_quantize(X, transposed=False, out: Mx | None = None) -> Mx:
 
 def ec_mx_dequantize(q: Mx, dtype=torch.bfloat16, out=None):
     """The values that q stands for, [..., rows, cols] of `dtype` (out's, when it is given)."""
-    dev, shape = q.codes.device, tuple(q.codes.shape[:-1]) + (q.cols,)
-    stream = _stream_of("ec_mx_dequantize", dev)
+    dev, stream = _device_of("ec_mx_dequantize", q.codes)
+    shape = tuple(q.codes.shape[:-1]) + (q.cols,)
     out = torch.empty(shape, dtype=dtype, device=dev) if out is None else out
     dt = _dtype_code("ec_mx_dequantize", out.dtype)
     c, s = _mx_operands("ec_mx_dequantize", dev, q, shape)
@@ -442,12 +444,12 @@ def ec_mx_dequantize(q: Mx, dtype=torch.bfloat16, out=None):
 
 def ec_mx_dispatch(cfg, X, place, out: Mx | None = None) -> Mx:
     """ec_dispatch with rows in the 4-bit format: [n * per_token, d_model]; rows that no choice holds are left as they were."""
-    dev, n, K, d = X.device, cfg.n, cfg.per_token, cfg.d_model
-    stream = _stream_of("ec_mx_dispatch", dev)
+    dev, stream = _device_of("ec_mx_dispatch", X)
+    n, K, d = cfg.n, cfg.per_token, cfg.d_model
     out = alloc_mx((n * K, d), dev) if out is None else out
     x, p = _dense("ec_mx_dispatch", dev, (X, _TYPES[cfg.dtype], (n, d)), (place, torch.int32, (n, K)))
     q, s = _mx_operands("ec_mx_dispatch", dev, out, (n * K, d))
-    _check(lib().ec_mx_dispatch(C.byref(cfg), x, p, q, s, stream), "ec_mx_dispatch")
+    _check(lib().ec_mx_dispatch(cfg, x, p, q, s, stream), "ec_mx_dispatch")
     return out
 
 
@@ -458,8 +460,8 @@ def ec_mx_expert_gemm(A: Mx, W: Mx, offsets, bias=None, act="none", out=None, dt
     """act(A[r] . W[e]^T + bias[e]) for the rows offsets[e] <= r < offsets[e + 1]: A [rows, K], W [E, N, K].  out: a tensor [rows, N] (None:
     a new one of `dtype`) or an Mx to receive the result in the 4-bit format.  act: "none", "erf" or "tanh" (GeLU).  Rows of no
     expert are left as they were."""
-    what, dev, (rows, _), (E, N, _), K = "ec_mx_expert_gemm", A.codes.device, A.codes.shape, W.codes.shape, W.cols
-    stream = _stream_of(what, dev)
+    what, (rows, _), (E, N, _), K = "ec_mx_expert_gemm", A.codes.shape, W.codes.shape, W.cols
+    dev, stream = _device_of(what, A.codes)
     out = torch.empty(rows, N, dtype=dtype, device=dev) if out is None else out
     ws = torch.empty(EC_MX_WORKSPACE_BYTES, dtype=torch.uint8, device=dev) if ws is None else ws
     a, sa = _mx_operands(what, dev, A, (rows, K))
@@ -475,7 +477,7 @@ def ec_mx_expert_gemm(A: Mx, W: Mx, offsets, bias=None, act="none", out=None, dt
         bt = _dtype_code(what, bias.dtype)
         bp, = _dense(what, dev, (bias, bias.dtype, (E, N)))
     cfg = ec_mx_gemm_config(rows, N, K, E, kind, _ACTS[act], bt)
-    _check(lib().ec_mx_expert_gemm(C.byref(cfg), a, sa, o, b, sb, bp, c, sc, w, ws.numel(), stream), what)
+    _check(lib().ec_mx_expert_gemm(cfg, a, sa, o, b, sb, bp, c, sc, w, ws.numel(), stream), what)
     return out
 
 

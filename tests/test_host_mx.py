@@ -88,7 +88,7 @@ def test_tensors_that_are_refused():
         with pytest.raises(B.EcError) as e:
             call()
         assert e.value.code == BAD
-    dev = torch.device("cpu")
+    dev = -1                                              # what torch says of a host tensor
     assert len(B._mx_operands("x", dev, q, (8, 64))) == 2
     for shape in ((8, 65), (8, 96), (4, 64), (1, 8, 64)):
         with pytest.raises(B.EcError):

@@ -77,10 +77,13 @@ def test_tensors_that_are_not_the_current_device_s():
 
 def test_operands_are_looked_at():
     """Types, shapes and layouts, before an address leaves for the library."""
-    dev = torch.device("cpu")
+    dev = -1                                              # what torch says of a host tensor
     i32, x = torch.int32, torch.zeros(16, 64)
     assert B._dense("x", dev, (x, torch.float32, (16, 64))) == [x.data_ptr()]
     for t, dtype, shape in ((x, torch.bfloat16, (16, 64)), (x, torch.float32, (64, 16)), (x.t(), torch.float32, (64, 16)), (x[:, ::2], torch.float32, (16, 32)),
-                            (x, i32, (16, 64)), (torch.zeros(16, 64, device="meta"), torch.float32, (16, 64))):
+                            (x, i32, (16, 64))):
         with pytest.raises(B.EcError):
             B._dense("x", dev, (t, dtype, shape))
+    for t in (x, torch.zeros(16, 64, device="meta")):     # not on device 0
+        with pytest.raises(B.EcError):
+            B._dense("x", 0, (t, torch.float32, (16, 64)))
