@@ -26,6 +26,7 @@
 #include "tc_ptx.cuh"
 
 #include <cudaTypedefs.h>
+#include <math.h>
 #include <string.h>
 
 namespace ecmoe {
@@ -43,18 +44,20 @@ constexpr int kTmemCols = 512;
 constexpr int kScaleStages = 2, kScaleStageK = 1024, kScaleRow = kScaleStageK / 32;
 constexpr int kSmemBudget = 221 * 1024;
 
-__host__ __device__ constexpr int scale_stage_bytes(int nt) { return (kM + nt) * kScaleRow; }
+// mt: MMAs side by side, 128 columns of C each
+__host__ __device__ constexpr int stage_bytes(int nt, int mt) { return mt * kBBytes + nt * kRowBytes; }
+__host__ __device__ constexpr int scale_stage_bytes(int nt, int mt) { return (mt * kM + nt) * kScaleRow; }
 // Most CTAs to a tile, and what the first of them keeps for the others' accumulators
 __host__ __device__ constexpr int most_split(int nt) { return nt == 32 ? 4 : nt == 64 ? 2 : 1; }
 __host__ __device__ constexpr int parts_bytes(int nt, bool split) { return split ? (most_split(nt) - 1) * kM * nt * 4 : 0; }
-__host__ __device__ constexpr int stages_of(int nt, bool split) {
-  const int fit = (kSmemBudget - parts_bytes(nt, split) - kScaleStages * scale_stage_bytes(nt)) / (kBBytes + nt * kRowBytes);
+__host__ __device__ constexpr int stages_of(int nt, bool split, int mt) {
+  const int fit = (kSmemBudget - parts_bytes(nt, split) - kScaleStages * scale_stage_bytes(nt, mt)) / stage_bytes(nt, mt);
   return fit > 10 ? 10 : fit;
 }
 // Columns of tensor memory for 128 of the contraction of A's scales, and for a stage's of both.  tcgen05.mma wants a scale matrix to begin
 // at a multiple of four columns, so narrow tiles leave some of the four unused.
 __host__ __device__ constexpr int cols_a(int nt) { return nt <= 128 ? 4 : 8; }
-__host__ __device__ constexpr int scale_cols(int nt) { return 8 + 2 * cols_a(nt); }
+__host__ __device__ constexpr int scale_cols(int nt, int mt) { return 8 * mt + 2 * cols_a(nt); }
 
 // TMA boxes a stage's rows of A come in
 __host__ __device__ constexpr int boxes_of(int nt) { return nt >= 128 ? 2 : 1; }
@@ -209,13 +212,14 @@ struct Walk {
   }
 };
 
-template <int NT, int OUT, bool SPLIT>
+template <int NT, int OUT, bool SPLIT, int MT>
 __global__ void __launch_bounds__(kThreads, 1)
 gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmAs,
                const __grid_constant__ CUtensorMap tmBs, const MxParams p) {
-  constexpr int S = stages_of(NT, SPLIT), kStage = kBBytes + NT * kRowBytes, kScaleStage = scale_stage_bytes(NT);
+  constexpr int S = stages_of(NT, SPLIT, MT), kStage = stage_bytes(NT, MT), kScaleStage = scale_stage_bytes(NT, MT);
+  constexpr int kTileM = MT * kM, kAt = MT * kBBytes, kBuffers = MT == 1 ? 2 : 1;    // A behind B in a stage; accumulators
   constexpr int kBoxes = boxes_of(NT), kBoxBytes = NT / kBoxes * kRowBytes;
-  constexpr int kColsA = cols_a(NT), kScaleCols = scale_cols(NT), kScales0 = 2 * NT;
+  constexpr int kColsA = cols_a(NT), kScaleCols = scale_cols(NT, MT), kScales0 = kBuffers * MT * NT;
   static_assert(kScales0 + S * kScaleCols <= kTmemCols, "tensor memory");
   static_assert(kScales0 % 4 == 0 && kScaleCols % 4 == 0 && kColsA % 4 == 0, "where a scale matrix may begin");
   extern __shared__ uint8_t smem_raw[];
@@ -298,7 +302,7 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     Walk<NT> walk(groups, p.tiles_m, first_tile);    // of A only the halves of a tile that hold rows are loaded
     for (int tile = first_tile, step = 0; tile < last_tile; tile += tile_step, step = tile_step) {
       walk.next(step);
-      const int e = __shfl_sync(0xffffffffu, walk.e, 0), col0 = __shfl_sync(0xffffffffu, walk.m, 0) * kM, row0 = __shfl_sync(0xffffffffu, walk.row0, 0);
+      const int e = __shfl_sync(0xffffffffu, walk.e, 0), col0 = __shfl_sync(0xffffffffu, walk.m, 0) * kTileM, row0 = __shfl_sync(0xffffffffu, walk.row0, 0);
       const int boxes = __shfl_sync(0xffffffffu, walk.rows > NT / kBoxes ? kBoxes : 1, 0);
       for (int kb = kb0; kb < kb1; ++kb) {
         if (kb % kUnit == 0) {
@@ -307,16 +311,16 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           const uint32_t sc = scale_base + scale_stage * kScaleStage, bar = ssf0 + 8 * scale_stage;
           expect_tx_if(lead, bar, kScaleStage);
           tma_load_3d_if(lead, sc, &tmBs, bar, kb * (kStageK / 32), col0, e);
-          tma_load_2d_if(lead, sc + kM * kScaleRow, &tmAs, bar, kb * (kStageK / 32), row0);
+          tma_load_2d_if(lead, sc + kTileM * kScaleRow, &tmAs, bar, kb * (kStageK / 32), row0);
           if (++scale_stage == kScaleStages) { scale_stage = 0; scale_phase ^= 1; }
         }
         wait(alive, empty0 + 8 * stage, phase ^ 1, abort_flag, p.status, 1);
         const uint32_t lead = elected & alive;
         const uint32_t sb = smem_base + stage * kStage, bar = full0 + 8 * stage;
-        expect_tx_if(lead, bar, kBBytes + boxes * kBoxBytes);
+        expect_tx_if(lead, bar, kAt + boxes * kBoxBytes);
         tma_load_3d_if(lead, sb, &tmB, bar, kb * kRowBytes, col0, e);
-        tma_load_2d_if(lead, sb + kBBytes, &tmA, bar, kb * kRowBytes, row0);
-        if constexpr (kBoxes == 2) tma_load_2d_if(boxes == 2 ? lead : 0u, sb + kBBytes + kBoxBytes, &tmA, bar, kb * kRowBytes, row0 + NT / 2);
+        tma_load_2d_if(lead, sb + kAt, &tmA, bar, kb * kRowBytes, row0);
+        if constexpr (kBoxes == 2) tma_load_2d_if(boxes == 2 ? lead : 0u, sb + kAt + kBoxBytes, &tmA, bar, kb * kRowBytes, row0 + NT / 2);
         if (++stage == S) { stage = 0; phase ^= 1; }
       }
     }
@@ -330,19 +334,21 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     for (int tile = first_tile, step = 0; tile < total; tile += tile_step, step = tile_step, ++it) {
       walk.next(step);
       const uint32_t idesc = __shfl_sync(0xffffffffu, idesc0 | ((uint32_t)(walk.rows + 31) / 32 << 19), 0);
-      const uint32_t buf = it & 1, d = buf * NT;
-      wait(alive, acce0 + 8 * buf, ((it >> 1) & 1) ^ 1, abort_flag, p.status, 2);
+      const uint32_t buf = kBuffers == 2 ? it & 1 : 0, use = kBuffers == 2 ? it >> 1 : it, d = buf * NT;
+      wait(alive, acce0 + 8 * buf, (use & 1) ^ 1, abort_flag, p.status, 2);
       for (int kb = kb0; kb < kb1; ++kb) {
         wait(alive, full0 + 8 * stage, phase, abort_flag, p.status, 4);
         tc_fence_after();
         const uint32_t lead = elected & alive;
-        const uint32_t scales = kScales0 + stage * kScaleCols, blow = low0 + stage * (kStage >> 4), alow = blow + (kBBytes >> 4);
+        const uint32_t scales = kScales0 + stage * kScaleCols, blow = low0 + stage * (kStage >> 4), alow = blow + (kAt >> 4);
         const int blocks = p.blocks - 8 * kb;        // left of the contraction; an MMA takes two
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const uint32_t half = 2 * (i & 1);
-          tc_mma_mx_if(blocks > 2 * i ? lead : 0u, d, blow + 2 * i, alow + 2 * i, idesc | (half << 4) | (half << 29), scales + 4 * (i >> 1),
-                       scales + 8 + kColsA * (i >> 1), (kb - kb0 | i) != 0);
+#pragma unroll
+          for (int h = 0; h < MT; ++h)
+            tc_mma_mx_if(blocks > 2 * i ? lead : 0u, d + h * NT, blow + h * (kBBytes >> 4) + 2 * i, alow + 2 * i, idesc | (half << 4) | (half << 29),
+                         scales + 8 * h + 4 * (i >> 1), scales + 8 * MT + kColsA * (i >> 1), (kb - kb0 | i) != 0);
         }
         tc_commit_if(lead, empty0 + 8 * stage);
         if (++stage == S) { stage = 0; phase ^= 1; }
@@ -360,21 +366,21 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         if (part == 0 && !warp_wait(ssf0 + 8 * scale_stage, scale_phase, abort_flag, p.status, 8, lane)) { gave_up = true; break; }
         // a row's eight bytes of this stage; the TMA unit's 32-byte swizzle exchanges the 16-byte halves of every other four rows
         const uint32_t from = scale_base + scale_stage * kScaleStage + lane * kScaleRow + (((part >> 1) ^ ((lane >> 2) & 1)) << 4) + 8 * (part & 1);
-        uint32_t v[kScaleCols];                      // as they lie in tensor memory: B's first 128 of the contraction, its second, A's first, its second
+        uint32_t v[kScaleCols];                      // as they lie in tensor memory: of each 128 columns B's first 128 of the contraction, its second; A's first, its second
 #pragma unroll
-        for (int i = 0; i < 4 + kRows; ++i) {
-          const int at = i < 4 ? i : 4 + i, half = i < 4 ? 4 : kColsA;
+        for (int i = 0; i < 4 * MT + kRows; ++i) {
+          const int at = i < 4 * MT ? 8 * (i / 4) + i % 4 : 4 * MT + i, half = i < 4 * MT ? 4 : kColsA;
           asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v[at]), "=r"(v[at + half]) : "r"(from + 32 * i * kScaleRow) : "memory");
         }
 #pragma unroll
-        for (int i = kRows; i < kColsA; ++i) v[8 + i] = v[8 + kColsA + i] = 0;
+        for (int i = kRows; i < kColsA; ++i) v[8 * MT + i] = v[8 * MT + kColsA + i] = 0;
         const int blocks = p.blocks - 8 * kb;
         if (blocks < 8) {                            // behind the contraction's end: whatever lies there becomes 0, 2^-127
           const uint32_t first = blocks >= 4 ? 0xFFFFFFFFu : 0xFFFFFFFFu >> (32 - 8 * blocks), second = blocks > 4 ? 0xFFFFFFFFu >> (64 - 8 * blocks) : 0u;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) { v[i] &= first; v[4 + i] &= second; }
+          for (int i = 0; i < 4 * MT; ++i) { v[8 * (i / 4) + i % 4] &= first; v[8 * (i / 4) + 4 + i % 4] &= second; }
 #pragma unroll
-          for (int i = 0; i < kColsA; ++i) { v[8 + i] &= first; v[8 + kColsA + i] &= second; }
+          for (int i = 0; i < kColsA; ++i) { v[8 * MT + i] &= first; v[8 * MT + kColsA + i] &= second; }
         }
         if (part == kUnit - 1 || kb + 1 == kb1) {     // all of these scales are in registers
           __syncwarp();
@@ -399,13 +405,16 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     int it = 0;
     Walk<NT> walk(groups, p.tiles_m, first_tile);
     for (int step = 0; walk.next(step); step = tile_step, ++it) {
-      const int buf = it & 1; const uint32_t use = (uint32_t)(it >> 1);
-      const int col = walk.m * kM + q * 32 + lane, rows = walk.rows;
-      const bool in = col < p.N;
-      float bias = 0.f;
-      if (p.bias != nullptr && in) {
-        const int64_t at = (int64_t)walk.e * p.N + col;
-        bias = p.bias_f32 ? __ldg((const float*)after_enter(p.bias) + at) : __bfloat162float(__ldg((const bf16*)after_enter(p.bias) + at));
+      const int buf = kBuffers == 2 ? it & 1 : 0, rows = walk.rows; const uint32_t use = (uint32_t)(kBuffers == 2 ? it >> 1 : it);
+      float biases[MT];
+#pragma unroll
+      for (int h = 0; h < MT; ++h) {
+        const int col = walk.m * kTileM + h * kM + q * 32 + lane;
+        biases[h] = 0.f;
+        if (p.bias != nullptr && col < p.N) {
+          const int64_t at = (int64_t)walk.e * p.N + col;
+          biases[h] = p.bias_f32 ? __ldg((const float*)after_enter(p.bias) + at) : __bfloat162float(__ldg((const bf16*)after_enter(p.bias) + at));
+        }
       }
       if (!warp_wait(accf0 + 8 * buf, use & 1, abort_flag, p.status, 6, lane)) { gave_up = true; break; }
       tc_fence_after();
@@ -432,8 +441,12 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         if (!cluster_wait(partf, it & 1, abort_flag, p.status, 11, lane)) { gave_up = true; break; }
       }
 #pragma unroll 1
-      for (int c = first; c < rows; c += kChunk * (kEpi / 4)) {     // uniform across the warp
-        uint32_t r[kChunk]; tc_ld16(taddr + c, r);
+      for (int c = first, h = 0; h < MT; c += kChunk * (kEpi / 4)) {         // uniform across the warp
+        if (c >= rows) { c = first - kChunk * (kEpi / 4); ++h; continue; }
+        const int col = walk.m * kTileM + h * kM + q * 32 + lane;
+        const bool in = col < p.N;
+        const float bias = biases[MT == 1 ? 0 : h];
+        uint32_t r[kChunk]; tc_ld16(taddr + h * NT + c, r);
         float v[kChunk];
 #pragma unroll
         for (int j = 0; j < kChunk; ++j) v[j] = __uint_as_float(r[j]);
@@ -481,7 +494,7 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           // The warp's 32 columns are one block of every row: the largest magnitude by one reduction per row, eight rows' codes turned
           // between the lanes (lane 8 i + j ends with columns 8 i .. 8 i + 7 of row j).  Columns behind the last are zeros: TMA fills their
           // weights with them.
-          const int block = walk.m * 4 + q;
+          const int block = (walk.m * MT + h) * 4 + q;
 #pragma unroll
           for (int j0 = 0; j0 < kChunk; j0 += 8) {
             float y[8];
@@ -545,19 +558,20 @@ bool byte_map(CUtensorMap* tm, const void* base, int dims, int64_t inner, int64_
 // No more row tiles than these: every expert may add one that is not full
 int64_t most_tiles(const MxGemmArgs& g, int nt) { return (g.rows - 1) / nt + (g.E < g.rows ? g.E : g.rows); }
 
-template <int NT, int OUT, bool SPLIT>
+template <int NT, int OUT, bool SPLIT, int MT = 1>
 cudaError_t launch_one(const MxGemmArgs& g, MxParams p, int sms, cudaStream_t st) {
   CUtensorMap ta, tb, tas, tbs;
   const int64_t inner = 16 * (int64_t)p.blocks, pitch = 16 * (int64_t)((g.K + 511) / 512);
   if (!byte_map(&ta, g.A, 2, inner, g.rows, 1, kRowBytes, NT / boxes_of(NT), CU_TENSOR_MAP_SWIZZLE_128B) ||
-      !byte_map(&tb, g.B, 3, inner, g.N, g.E, kRowBytes, kM, CU_TENSOR_MAP_SWIZZLE_128B) ||
+      !byte_map(&tb, g.B, 3, inner, g.N, g.E, kRowBytes, MT * kM, CU_TENSOR_MAP_SWIZZLE_128B) ||
       !byte_map(&tas, g.A_scales, 2, pitch, g.rows, 1, kScaleRow, NT, CU_TENSOR_MAP_SWIZZLE_32B) ||
-      !byte_map(&tbs, g.B_scales, 3, pitch, g.N, g.E, kScaleRow, kM, CU_TENSOR_MAP_SWIZZLE_32B)) return cudaErrorInvalidValue;
-  constexpr int S = stages_of(NT, SPLIT);
-  constexpr int smem = S * (kBBytes + NT * kRowBytes) + kScaleStages * scale_stage_bytes(NT) + parts_bytes(NT, SPLIT) + 1024 + (2 * S + 7 + 2 * kScaleStages) * 8 +
+      !byte_map(&tbs, g.B_scales, 3, pitch, g.N, g.E, kScaleRow, MT * kM, CU_TENSOR_MAP_SWIZZLE_32B)) return cudaErrorInvalidValue;
+  constexpr int S = stages_of(NT, SPLIT, MT);
+  p.tiles_m = (g.N + MT * kM - 1) / (MT * kM);
+  constexpr int smem = S * stage_bytes(NT, MT) + kScaleStages * scale_stage_bytes(NT, MT) + parts_bytes(NT, SPLIT) + 1024 + (2 * S + 7 + 2 * kScaleStages) * 8 +
                        (int)sizeof(Groups);
   static_assert(smem <= 227 * 1024, "shared memory");
-  auto kern = gemm_mx_kernel<NT, OUT, SPLIT>;
+  auto kern = gemm_mx_kernel<NT, OUT, SPLIT, MT>;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   const int64_t most = most_tiles(g, NT) * p.tiles_m, at_once = sms / p.split;
@@ -577,6 +591,16 @@ cudaError_t launch_narrow(const MxGemmArgs& g, MxParams p, int sms, cudaStream_t
   p.split = pick_split(g, p, NT, sms);
   return p.split > 1 ? launch_one<NT, OUT, true>(g, p, sms, st) : launch_one<NT, OUT, false>(g, p, sms, st);
 }
+// 256 columns of C per tile instead of 128, where one accumulator for both halves leaves the epilogue in the open: a stage then takes 1028
+// cycles for two MMAs side by side instead of 775 for one (an SM receives 52 of its 54 bytes a clock with the narrow tiles, 56 KiB instead of
+// 80 for the same work here), the epilogue some 2700 per 128 columns, 5200 with GeLU, 7000 to 4 bits.  The fewest cycles for the
+// number of tiles to expect, an expert's last being half full.  Measured: 32768 rows, 64 experts, 4096 x 16384, at the power cap 1538 -> 1445 us;
+// 3062 rows, 16 experts, 4072 x 1096, 23.5 -> 19.2; 8192 x 4096 to 4 bits 175 -> 161; not taken: 2048 x 4096 53 and 66, 768 x 2048 33 and 45.
+bool wide(const MxGemmArgs& g, const MxParams& p, int sms) {
+  const double tiles = g.rows / 192.0 + 0.5 * g.E, epi = g.out == EC_MX_OUT_MX ? 7000 : g.act != EC_MX_NONE ? 5200 : 2700;
+  auto rounds = [&](int cols) { return ceil(tiles * ((g.N + cols - 1) / cols) / sms); };
+  return rounds(256) * (p.kblocks * 1028.0 + 2 * epi + 1500) < rounds(128) * fmax(p.kblocks * 775.0 + 700, epi + 1100);
+}
 template <int OUT>
 cudaError_t launch_out(const MxGemmArgs& g, const MxParams& p, int sms, cudaStream_t st) {
   // Rows per tile.  A tile of 64, 128 or 192 rows takes nearly the same time (64 experts of 4096 x 16384: 350, 396 and 434 us per row tile of
@@ -586,7 +610,8 @@ cudaError_t launch_out(const MxGemmArgs& g, const MxParams& p, int sms, cudaStre
   const int64_t mean = g.rows / g.E;
   if (mean <= 2) return launch_narrow<32, OUT>(g, p, sms, st);     // eight rows of one token each: 64 us, with tiles of 64 rows 72 (more of the weights on their way)
   if (mean <= 20) return launch_narrow<64, OUT>(g, p, sms, st);
-  return mean <= 90 ? launch_one<128, OUT, false>(g, p, sms, st) : launch_one<192, OUT, false>(g, p, sms, st);
+  if (mean <= 90) return launch_one<128, OUT, false>(g, p, sms, st);
+  return wide(g, p, sms) ? launch_one<192, OUT, false, 2>(g, p, sms, st) : launch_one<192, OUT, false>(g, p, sms, st);
 }
 
 }  // namespace

@@ -132,7 +132,7 @@ PRODUCTS = [                                              # rows, N, K, E, group
     (31, 128, 544, 1, "even"), (32, 256, 1024, 1, "even"), (33, 128, 288, 1, "even"), (64, 264, 320, 1, "even"), (65, 128, 96, 1, "even"),
     (129, 128, 1000, 1, "even"), (193, 136, 776, 1, "even"), (192, 128, 4096, 1, "even"), (400, 40, 520, 3, "any"), (700, 384, 264, 5, "any"),
     (777, 520, 1032, 7, "tail"), (300, 72, 40, 256, "any"), (300, 128, 128, 4, "none"), (1500, 128, 64, 2, "one"), (1024, 1096, 512, 16, "even"),
-    (2000, 256, 2056, 9, "any"),
+    (2000, 256, 2056, 9, "any"), (4000, 1096, 4104, 2, "any"), (2900, 2000, 5000, 3, "tail"),
 ]
 
 
@@ -167,7 +167,7 @@ def test_sums_that_fp32_holds_are_exact(rows, N, K, E):
     assert np.array_equal(_np(out), M.product(a, w, offsets)[0])
 
 
-@pytest.mark.parametrize("rows,N,K,E", [(9, 136, 520, 4), (100, 256, 128, 1), (200, 1000, 96, 1), (500, 72, 1000, 2)])
+@pytest.mark.parametrize("rows,N,K,E", [(9, 136, 520, 4), (100, 256, 128, 1), (200, 1000, 96, 1), (500, 72, 1000, 2), (4000, 1096, 8200, 2)])
 @pytest.mark.parametrize("act", ["none", "erf", "tanh"])
 def test_bias_activation_and_each_result_type(rows, N, K, E, act):
     A, W, a, w = _case(rows, N, K, E, N, spread=1)
