@@ -378,8 +378,8 @@ typedef struct {
  * C[r, :] = act(A[r, :] . B[e]^T + bias[e, :]) for the rows offsets[e] <= r < offsets[e + 1] of expert e: groups of any length,
  * also none.  A [rows, K] and B [E, N, K] in the format above, offsets [E + 1] as ec_sort_tokens writes them (or i * k for the slots
  * of expert choice), bias [E, N] or NULL; C [rows, N] fp32 or bf16, dense, or the codes of the result as blocks along N with its scales
- * in C_scales (NULL otherwise), ready to be the next product's A.  Products are exact, sums fp32, bias and act fp32, one rounding.  Rows
- * of no expert are left as they were.  offsets that decrease or leave [0, rows] are read as if cut to that range: every access
+ * in C_scales (NULL otherwise), ready to be the next product's A.  Products are exact, sums fp32 (in an order that depends on the call's
+ * sizes alone; what is below fp32's normal range may count as zero), bias and act fp32, one rounding.  Rows of no expert are left as they were.  offsets that decrease or leave [0, rows] are read as if cut to that range: every access
  * stays inside the arrays.  rows = 0: nothing to do.  `ws`: 256 bytes, 256-byte aligned, for the status word (ec_read_status).
  */
 #define EC_MX_WORKSPACE_BYTES 256

@@ -16,6 +16,12 @@
 //                prepared layout could serve them.
 // Few rows leave few tiles: then a cluster of CTAs shares each (SPLIT), each a stretch of the contraction, and the first adds up the others'
 // accumulators, which they write into its shared memory, in the order of the stretches.
+// MT = 2: two MMAs side by side, 256 columns of C, for long contractions (see wide()); the one accumulator's halves are handed over one by one
+// (32768 rows, 4096 x 16384, at the power cap: 1432 us, both at once 1471).
+// What bounds it: few rows, the reading of the weights (64 experts of 4096 x 16384, 32 rows each, 377 us, 92 % of the copy rate; eight rows of eight
+// experts 53 us, 82 %); many rows, the issuing warps and the 54 bytes a clock an SM receives from L2, then the board's 1000 W (32768 rows: 1190 us
+// alone, 1430 in a loop, 3.0 to 3.7 PFLOP/s); short contractions, the epilogue (16384 rows, 768 x 2048: 33 us, with GeLU 55, of which 17 are
+// the multiply-adds of the polynomial at full rate, to 4 bits 67).
 // Two accumulators of NT columns, and as many buffers of scales as there are stages: a stage is full when its operands have landed and
 // its scales are in tensor memory, and one commit frees both.  (A wait that is over at once still takes the MMA warp 100 cycles, a commit
 // 60 to 100, issuing an MMA 80: with barriers of their own for the scales a stage took 815 cycles beside the MMAs' 384.)
@@ -224,7 +230,7 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   static_assert(kScales0 % 4 == 0 && kScaleCols % 4 == 0 && kColsA % 4 == 0, "where a scale matrix may begin");
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  // barriers: full[S], empty[S], of the accumulators full[2], empty[2], of the scales in shared memory the same
+  // barriers: full[S], empty[S], of the accumulators full[2], empty[2] (MT = 2: of its halves), of the scales in shared memory the same
   // and, of the parts of a split tile, full and empty
   uint64_t* bars = (uint64_t*)(smem + S * kStage + kScaleStages * kScaleStage + parts_bytes(NT, SPLIT));
   uint32_t* tmem_slot = (uint32_t*)(bars + 2 * S + 6 + 2 * kScaleStages);
@@ -335,22 +341,46 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       walk.next(step);
       const uint32_t idesc = __shfl_sync(0xffffffffu, idesc0 | ((uint32_t)(walk.rows + 31) / 32 << 19), 0);
       const uint32_t buf = kBuffers == 2 ? it & 1 : 0, use = kBuffers == 2 ? it >> 1 : it, d = buf * NT;
-      wait(alive, acce0 + 8 * buf, (use & 1) ^ 1, abort_flag, p.status, 2);
-      for (int kb = kb0; kb < kb1; ++kb) {
-        wait(alive, full0 + 8 * stage, phase, abort_flag, p.status, 4);
-        tc_fence_after();
+      // MMAs of one stage, of the halves h0 .. h1 - 1
+      auto issue = [&](int kb, uint32_t st, int h0, int h1) {
         const uint32_t lead = elected & alive;
-        const uint32_t scales = kScales0 + stage * kScaleCols, blow = low0 + stage * (kStage >> 4), alow = blow + (kAt >> 4);
+        const uint32_t scales = kScales0 + st * kScaleCols, blow = low0 + st * (kStage >> 4), alow = blow + (kAt >> 4);
         const int blocks = p.blocks - 8 * kb;        // left of the contraction; an MMA takes two
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const uint32_t half = 2 * (i & 1);
 #pragma unroll
           for (int h = 0; h < MT; ++h)
-            tc_mma_mx_if(blocks > 2 * i ? lead : 0u, d + h * NT, blow + h * (kBBytes >> 4) + 2 * i, alow + 2 * i, idesc | (half << 4) | (half << 29),
-                         scales + 8 * h + 4 * (i >> 1), scales + 8 * MT + kColsA * (i >> 1), (kb - kb0 | i) != 0);
+            if (h0 <= h && h < h1)
+              tc_mma_mx_if(blocks > 2 * i ? lead : 0u, d + h * NT, blow + h * (kBBytes >> 4) + 2 * i, alow + 2 * i, idesc | (half << 4) | (half << 29),
+                           scales + 8 * h + 4 * (i >> 1), scales + 8 * MT + kColsA * (i >> 1), (kb - kb0 | i) != 0);
         }
-        tc_commit_if(lead, empty0 + 8 * stage);
+      };
+      wait(alive, acce0 + 8 * buf, (use & 1) ^ 1, abort_flag, p.status, 2);
+      int kb = kb0;
+      if constexpr (MT == 2) {
+        // The first half of the accumulator is free before the second: the stages at hand are multiplied into it meanwhile.
+        const int some = min(kb0 + S, kb1);
+        uint32_t st = stage, ph = phase;
+        for (; kb < some; ++kb) {
+          wait(alive, full0 + 8 * st, ph, abort_flag, p.status, 4);
+          tc_fence_after();
+          issue(kb, st, 0, 1);
+          if (++st == S) { st = 0; ph ^= 1; }
+        }
+        wait(alive, acce0 + 8, (use & 1) ^ 1, abort_flag, p.status, 2);
+        tc_fence_after();
+        for (int k = kb0; k < some; ++k) {
+          issue(k, stage, 1, 2);
+          tc_commit_if(elected & alive, empty0 + 8 * stage);
+          if (++stage == S) { stage = 0; phase ^= 1; }
+        }
+      }
+      for (; kb < kb1; ++kb) {
+        wait(alive, full0 + 8 * stage, phase, abort_flag, p.status, 4);
+        tc_fence_after();
+        issue(kb, stage, 0, MT);
+        tc_commit_if(elected & alive, empty0 + 8 * stage);
         if (++stage == S) { stage = 0; phase ^= 1; }
       }
       tc_commit_if(elected & alive, accf0 + 8 * buf);
@@ -442,7 +472,15 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       }
 #pragma unroll 1
       for (int c = first, h = 0; h < MT; c += kChunk * (kEpi / 4)) {         // uniform across the warp
-        if (c >= rows) { c = first - kChunk * (kEpi / 4); ++h; continue; }
+        if (c >= rows) {                             // done with this half of the columns
+          if constexpr (MT == 2) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(acce0 + 8 * h);
+          }
+          c = first - kChunk * (kEpi / 4); ++h;
+          continue;
+        }
         const int col = walk.m * kTileM + h * kM + q * 32 + lane;
         const bool in = col < p.N;
         const float bias = biases[MT == 1 ? 0 : h];
@@ -521,9 +559,11 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           }
         }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(acce0 + 8 * buf);
+      if constexpr (MT == 1) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(acce0 + 8 * buf);
+      }
       if constexpr (SPLIT) {                         // the parts have been read
         if (lane == 0) for (int other = 1; other < ctas; ++other) mbar_arrive_cluster(map_to_cta(parte, other));
       }

@@ -53,7 +53,8 @@ template <int L> __device__ __forceinline__ unsigned gather_scales(unsigned s, i
 
 // L = 32: a warp takes H times 256 columns of a row, lane i eight neighbouring values of each, so its loads and its 128 bytes of codes are
 // whole lines.  L = 4, 8, 16: rows of at most L / 4 blocks, 32 / L of them to a warp.  PLACED: the row is a token's and goes to every
-// row place[t, j] names.
+// row place[t, j] names.  Memory bounds the fp32 form (16384 x 4096 45.7 us, the copy rate); in bf16 a byte costs twice the
+// instructions: 31.9 us, 5.3 TB/s (H = 2: 37.4).  To two rows per token 39.3 us.  131072 x 64 7.2 us (with a warp per row 34).
 template <typename T, bool PLACED, int L, int H>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* X, int64_t rows, int64_t items, int stretches, int cols, uint8_t* codes, uint8_t* scales,
                                                             const int32_t* place, int K, int64_t out_rows) {
@@ -105,7 +106,8 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* X, int64_t 
 
 // X [batches][cols][rows], the contraction along its rows: output row r is column r of a matrix.  A CTA takes 256 of the contraction and
 // 64 columns; a warp one block of 32 of the contraction, lane i two neighbouring columns, so its 32 loads are 32 lines.  The codes
-// turn in shared memory and leave as 128 bytes of an output row at a time.
+// turn in shared memory and leave as 128 bytes of an output row at a time.  Memory bounds it: 4 x 4096 x 8192 bf16 58 us (89 % of the copy
+// rate; two CTAs per SM instead of three 70, loads unpacked one by one as they come 270), fp32 88 us.
 template <typename T>
 __global__ void __launch_bounds__(256, 3) quantize_columns_kernel(const T* X, int rows, int cols, int groups, uint8_t* codes, uint8_t* scales) {
   __shared__ uint4 tile[64][8 + 1];
@@ -160,7 +162,8 @@ __global__ void __launch_bounds__(256, 3) quantize_columns_kernel(const T* X, in
 
 // The codes of 16 bytes of values at a time: eight in bf16, four in fp32, so that a warp's stores are whole lines.  The three bits of a
 // magnitude, put where fp32 has the end of its exponent and the start of its fraction, are 2^-126 times what they stand for, the
-// subnormal ones among them.  Lanes as in the quantisation: L = 32, U times 32 pieces of a row; else 32 / L rows, U times.
+// subnormal ones among them.  Lanes as in the quantisation: L = 32, U times 32 pieces of a row; else 32 / L rows, U times.  Memory bounds it:
+// 16384 x 4096 to bf16 28 us (92 % of the copy rate), to fp32 48.5 (95 %).
 template <typename T, int L, int U>
 __global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t items, int stretches, int pieces,
                                                          int code_pitch, int scale_pitch, uint4* X) {

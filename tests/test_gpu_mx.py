@@ -214,6 +214,34 @@ def test_nan_and_what_lies_outside(rows):
     assert (q.scales[2:5, :4] != 255).all() and (q.scales[6:rows - 3, 5:7] != 255).all()
 
 
+@pytest.mark.parametrize("rows", [3, 40, 100, 250])
+def test_the_ends_of_the_range(rows):
+    """Scales at both ends: sums beyond fp32 are infinities of their sign, those below its normal range are off by at most 2^-126 per
+    product, and zeros times the largest scale stay zeros."""
+    K, N = 96, 136
+    g = torch.Generator().manual_seed(rows)
+    A, W = B.alloc_mx((rows, K)), B.alloc_mx((1, N, K))
+    for q in (A, W):
+        q.codes.copy_(torch.randint(0, 256, q.codes.shape, generator=g, dtype=torch.uint8))
+    W.codes &= 0x77                                       # no negative weights
+    A.codes[0] = 0x11; A.codes[1] = 0x99; W.codes[0, 0] = 0x22
+    off = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+
+    def run(a, w):
+        A.scales.fill_(a); W.scales.fill_(w)
+        return _np(B.ec_mx_expert_gemm(A, W, off, dtype=F32))
+
+    big = run(254, 254)
+    assert big[0, 0] == np.inf and big[1, 0] == -np.inf
+    plain = run(127, 127)
+    assert plain[0, 0] == K / 2 and plain[1, 0] == -K / 2
+    for a, w in ((60, 70), (1, 126), (0, 127), (0, 100), (0, 0), (1, 60)):
+        assert (np.abs(run(a, w) - np.ldexp(plain, a + w - 254)) <= K * 2.0 ** -126).all(), (a, w)
+    assert np.array_equal(run(150, 140), np.ldexp(plain, 36)) and np.array_equal(run(10, 244), plain)
+    A.codes.fill_(0x08)                                   # zeros of either sign
+    assert (run(254, 254) == 0).all()
+
+
 def test_offsets_are_cut_to_the_rows():
     """Offsets are the caller's memory: below 0 counts as 0, beyond the rows as their number, a decrease as an empty group."""
     rows, N, K, E = 150, 136, 64, 6
