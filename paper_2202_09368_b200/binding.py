@@ -460,7 +460,10 @@ def ec_mx_expert_gemm(A: Mx, W: Mx, offsets, bias=None, act="none", out=None, dt
     """act(A[r] . W[e]^T + bias[e]) for the rows offsets[e] <= r < offsets[e + 1]: A [rows, K], W [E, N, K].  out: a tensor [rows, N] (None:
     a new one of `dtype`) or an Mx to receive the result in the 4-bit format.  act: "none", "erf" or "tanh" (GeLU).  Rows of no
     expert are left as they were."""
-    what, (rows, _), (E, N, _), K = "ec_mx_expert_gemm", A.codes.shape, W.codes.shape, W.cols
+    what = "ec_mx_expert_gemm"
+    if A.codes.dim() != 2 or W.codes.dim() != 3 or act not in _ACTS:
+        raise EcError(EC_ERR_INVALID_ARG, f"{what}: wanted A [rows, K], W [E, N, K] and an act of {tuple(_ACTS)}, got {A.codes.dim()} and {W.codes.dim()} axes, {act!r}")
+    (rows, _), (E, N, _), K = A.codes.shape, W.codes.shape, W.cols
     dev, stream = _device_of(what, A.codes)
     out = torch.empty(rows, N, dtype=dtype, device=dev) if out is None else out
     ws = torch.empty(EC_MX_WORKSPACE_BYTES, dtype=torch.uint8, device=dev) if ws is None else ws

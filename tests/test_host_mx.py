@@ -88,6 +88,11 @@ def test_tensors_that_are_refused():
         with pytest.raises(B.EcError) as e:
             call()
         assert e.value.code == BAD
+    W, off = B.alloc_mx((2, 8, 64), "cpu"), torch.zeros(3, dtype=torch.int32)
+    for call in (lambda: B.ec_mx_expert_gemm(q, W, off, act="relu"), lambda: B.ec_mx_expert_gemm(q, q, off), lambda: B.ec_mx_expert_gemm(W, W, off)):
+        with pytest.raises(B.EcError) as e:
+            call()
+        assert e.value.code == BAD
     dev = -1                                              # what torch says of a host tensor
     assert len(B._mx_operands("x", dev, q, (8, 64))) == 2
     for shape in ((8, 65), (8, 96), (4, 64), (1, 8, 64)):
