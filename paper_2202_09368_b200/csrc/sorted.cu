@@ -262,9 +262,10 @@ template <typename T, int V> __device__ __forceinline__ typename Pack<T, V>::typ
 
 // KB rows of a token are on their way at a time, kPieces pieces of each; the sum runs over j in ascending order, in fp32, and is rounded once.
 // Memory bounds it, short rows the latency of place -> row: 16384 x 4096 bf16, two rows, 68 us (91 % of the copy rate); 65536 x 1024,
-// eight rows, 194 us (95 %); 8192 x 768 fp32 13.7 us (84 %); 6079 x 1000, three rows, 13.1 us (57 %); 262144 x 64, two, 31 us (49 %).
+// eight rows, 194 us (95 %); 8192 x 768 fp32 13.7 us (84 %); 6079 x 1000, three rows, 13.1 us (57 %); 262144 x 64, two, 24 us (64 %; with
+// room for four rows, whose registers hold up to a third of the warps, 31).
 template <typename T, typename TY, int G, int kPieces, int KB>
-__global__ void __launch_bounds__(256) combine_rows_kernel(const uint4* Y, const float* weights, const int32_t* place, void* X_out, int64_t items,
+__global__ void __launch_bounds__(256, G < 32 && KB == 2 ? 6 : 0) combine_rows_kernel(const uint4* Y, const float* weights, const int32_t* place, void* X_out, int64_t items,
                                                            int stretches, int pieces, int K, int64_t rows) {
   constexpr int V = Vec<TY>::V;
   using Out = typename Pack<T, V>::type;
@@ -428,9 +429,10 @@ cudaError_t combine_with(const void* Y, const float* w, const int32_t* place, vo
 template <typename T, typename TY>
 cudaError_t combine_of(const void* Y, const float* w, const int32_t* place, void* X_out, int64_t n, int d, int K, cudaStream_t st) {
   const int pieces = d / Vec<TY>::V;
+  // narrow rows, two to a token: 65536 x 120 bf16 12.9 us by twos, 16.5 by fours; three: 65536 x 64 fp32 16.7 and 15.0; four: 262144 x 64 35.4 and 35.7
   switch (group_of(pieces)) {
-    case 8: return combine_with<T, TY, 8, 1, 4>(Y, w, place, X_out, n, pieces, K, st);
-    case 16: return combine_with<T, TY, 16, 1, 4>(Y, w, place, X_out, n, pieces, K, st);
+    case 8: return K <= 2 ? combine_with<T, TY, 8, 1, 2>(Y, w, place, X_out, n, pieces, K, st) : combine_with<T, TY, 8, 1, 4>(Y, w, place, X_out, n, pieces, K, st);
+    case 16: return K <= 2 ? combine_with<T, TY, 16, 1, 2>(Y, w, place, X_out, n, pieces, K, st) : combine_with<T, TY, 16, 1, 4>(Y, w, place, X_out, n, pieces, K, st);
   }
   if (K == 1) return combine_with<T, TY, 32, 4, 1>(Y, w, place, X_out, n, pieces, K, st);
   return K == 2 ? combine_with<T, TY, 32, 2, 2>(Y, w, place, X_out, n, pieces, K, st) : combine_with<T, TY, 32, 1, 4>(Y, w, place, X_out, n, pieces, K, st);
