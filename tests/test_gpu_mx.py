@@ -32,7 +32,7 @@ def _special(rows, cols, dtype, seed):
     return x.to(dtype)
 
 
-SHAPES = [(1, 8), (3, 32), (5, 40), (7, 256), (64, 264), (9, 512), (33, 520), (130, 1000), (17, 2056), (4, 16384)]
+SHAPES = [(1, 8), (3, 32), (5, 40), (7, 64), (9, 72), (33, 128), (6, 136), (7, 256), (64, 264), (9, 512), (33, 520), (130, 1000), (17, 2056), (4, 16384)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -85,7 +85,7 @@ def test_no_rows():
     assert B.ec_mx_expert_gemm(B.ec_mx_quantize(torch.zeros(0, 64, device="cuda")), W, torch.zeros(3, dtype=torch.int32, device="cuda")).shape == (0, 8)
 
 
-@pytest.mark.parametrize("dtype,n,K,E,d", [(BF16, 1, 1, 4, 8), (BF16, 37, 3, 10, 1000), (F32, 64, 8, 16, 36), (F32, 5, 32, 256, 520), (BF16, 300, 2, 8, 4096)])
+@pytest.mark.parametrize("dtype,n,K,E,d", [(BF16, 1, 1, 4, 8), (BF16, 37, 3, 10, 1000), (F32, 50, 2, 4, 200), (BF16, 21, 2, 4, 120), (F32, 64, 8, 16, 36), (F32, 5, 32, 256, 520), (BF16, 300, 2, 8, 4096)])
 def test_dispatch_of_quantised_rows(dtype, n, K, E, d):
     """The bits of the quantised rows, at the places of a plan with holes; the other rows as they were."""
     g = torch.Generator().manual_seed(9)
