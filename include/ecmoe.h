@@ -301,7 +301,8 @@ ec_status ec_validate_routing(const ec_config* cfg, const int32_t* I, const int3
  * Restrictions (EC_ERR_UNSUPPORTED): rows of d_model elements of either type a multiple of 16 bytes, d_model <= 2^22 - 64,
  * 1 <= E <= 256, 1 <= per_token <= 32, n * per_token < 2^31.  n = 0 is a call: it writes offsets (zeros) and
  * nothing else, and its empty arguments may be NULL.  An output must not overlap an input or another output.  Any contents of
- * `choice` and of `place` are safe to pass: what lies outside its range counts as "no expert".
+ * `choice` and of `place` are safe to pass: what lies outside its range counts as "no expert".  ec_sort_tokens looks at its
+ * arrays and its scratch and refuses those that overlap (EC_ERR_INVALID_ARG).
  */
 typedef struct {
   int64_t n;         /* tokens                                                            */

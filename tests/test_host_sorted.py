@@ -1,5 +1,6 @@
 """What the calls on tokens sorted by expert refuse, and their size functions; nothing here reaches a GPU."""
 import ctypes as C
+import itertools
 
 import pytest
 import torch
@@ -55,6 +56,17 @@ def test_pointers():
     assert B.ec_sort_workspace_bytes(B.make_sort_config(1, 64, 256, 32)) <= 1 << 18
     for f in (L.ec_sort_workspace_bytes,):
         assert f(None) == 0
+
+
+@pytest.mark.parametrize("one,other", itertools.combinations(range(5), 2))
+@pytest.mark.parametrize("shift", [0, 16])
+def test_arrays_of_the_plan_that_overlap(one, other, shift):
+    """Two of choice, offsets, order, place and the workspace on one another: the kernels index shared memory and `order` by what they
+    read back of these, so the call is refused."""
+    cfg, L = B.make_sort_config(1 << 16, 64, 8, 2), B.lib()
+    args = [(i + 1) << 22 for i in range(5)]
+    args[one] = args[other] + shift
+    assert L.ec_sort_tokens(C.byref(cfg), *args, 1 << 18, None) == B.EC_ERR_INVALID_ARG
 
 
 def test_no_tokens():
