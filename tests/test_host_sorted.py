@@ -58,7 +58,7 @@ def test_pointers():
         assert f(None) == 0
 
 
-@pytest.mark.parametrize("one,other", itertools.combinations(range(5), 2))
+@pytest.mark.parametrize("one,other", list(itertools.combinations(range(5), 2)))
 @pytest.mark.parametrize("shift", [0, 16])
 def test_arrays_of_the_plan_that_overlap(one, other, shift):
     """Two of choice, offsets, order, place and the workspace on one another: the kernels index shared memory and `order` by what they
