@@ -158,7 +158,7 @@ def prepare(case, seed):
         s["b" + which] = normal((E, N), 0.5, torch.bfloat16 if case["op"] == "ffn" else DTYPES[case["dtype"]]) if case["bias"] else None
     if case["op"] == "ffn":
         s.update(X=normal((n, d), 1.0, torch.bfloat16), Xq=zeros((M, 16 * -(-d // 32)), torch.uint8), Xp=zeros((M, _pitch(d)), torch.uint8),
-                 Hq=zeros((M, 16 * -(-f // 32)), torch.uint8), Hp=zeros((M, _pitch(f)), torch.uint8), Y=zeros((M, d), torch.bfloat16),
+                 Hq=zeros((M, 16 * -(-f // 32)), torch.uint8), Hp=zeros((M, _pitch(f)), torch.uint8), Y=zeros((M, d), torch.float32),
                  X_out=zeros((n, d), torch.bfloat16))
     else:
         s.update(X=normal((M, d), 1.0, torch.bfloat16), Xq=zeros((M, 16 * -(-d // 32)), torch.uint8), Xp=zeros((M, _pitch(d)), torch.uint8),
@@ -275,12 +275,13 @@ def _framework(s):
         q = B.ec_mx_quantize(s["X"], out=B.Mx(s["Xq"], s["Xp"], s["d"]))
         return {"C": B.ec_mx_expert_gemm(q, B.Mx(s["W1"], s["S1"], s["d"]), s["offsets"], bias=s["b1"], act=s["act"], out=s["C"], ws=ws)}
     X, n, d, E, K = s["X"], s["n"], s["d"], s["E"], s["K"]
-    cfg = B.make_sort_config(n, d, E, K, X.dtype)
+    # the second product's rows stay in fp32 until the combine has added them up: one rounding, at the end
+    cfg = B.make_sort_config(n, d, E, K, X.dtype, torch.float32 if s["op"] == "ffn" else X.dtype)
     plan = B.ec_sort_tokens(cfg, s["choice"], out=B.Sorted(s["offsets"], s["order"], s["place"]), ws=ws)
     if s["op"] == "ffn":
         rows = B.ec_mx_dispatch(cfg, X, plan.place, out=B.Mx(s["Xq"], s["Xp"], d))
-        H = B.ec_mx_expert_gemm(rows, B.Mx(s["W1"], s["S1"], d), plan.offsets, bias=s["b1"], act=s["act"], out=B.Mx(s["Hq"], s["Hp"], s["f"]), ws=ws)
-        Y = B.ec_mx_expert_gemm(H, B.Mx(s["W2"], s["S2"], s["f"]), plan.offsets, bias=s["b2"], out=s["Y"], ws=ws)
+        H = B.ec_mx_expert_gemm(rows, B.Mx(s["W1"], s["S1"], d), plan.offsets, bias=s["b1"], act=s["act"], out=B.Mx(s["Hq"], s["Hp"], s["f"]), ws=ws[-512:-256])
+        Y = B.ec_mx_expert_gemm(H, B.Mx(s["W2"], s["S2"], s["f"]), plan.offsets, bias=s["b2"], out=s["Y"], ws=ws[-256:])         # each with a status word of its own
         return {"X_out": B.ec_combine(cfg, Y, s["weights"], plan.place, X_out=s["X_out"])}
     out = {"offsets": plan.offsets, "order": plan.order, "place": plan.place, "X_s": B.ec_dispatch(cfg, X, plan.place, X_s=s["X_s"]),
            "X_out": B.ec_combine(cfg, s["Y"], s["weights"], plan.place, X_out=s["X_out"])}
