@@ -321,7 +321,8 @@ size_t ec_sort_workspace_bytes(const ec_sort_config* cfg);
 ec_status ec_sort_tokens(const ec_sort_config* cfg, const int32_t* choice, int32_t* offsets, int32_t* order, int32_t* place,
                          void* ws, size_t ws_bytes, void* cuda_stream);
 
-/* X_s[place[t, j], :] = X[t, :] for every choice that names an expert.  Its gradient is ec_combine with weights = NULL. */
+/* X_s[place[t, j], :] = X[t, :] for every choice that names an expert.  Its gradient is ec_combine with weights = NULL and dX_s, whose type
+ * is X's, for Y: with a configuration whose y_dtype is its dtype (another y_dtype would read dX_s's rows as that type). */
 ec_status ec_dispatch(const ec_sort_config* cfg, const void* X, const int32_t* place, void* X_s, void* cuda_stream);
 
 /* X_out[t, :] = sum over j of weights[t, j] * Y[place[t, j], :], j ascending, accumulated in fp32 and rounded once; choices

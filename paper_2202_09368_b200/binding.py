@@ -351,9 +351,11 @@ def ec_dispatch(cfg, X, place, X_s=None):
 
 
 def ec_combine(cfg, Y, weights, place, X_out=None):
-    """X_out[t, :] = sum_j weights[t, j] * Y[place[t, j], :]; weights None: all ones."""
+    """X_out[t, :] = sum_j weights[t, j] * Y[place[t, j], :]; weights None: all ones, and Y may have X's type too (the gradient of ec_dispatch)."""
     dev, stream = _device_of("ec_combine", Y)
     n, K, d, dt = cfg.n, cfg.per_token, cfg.d_model, _TYPES[cfg.dtype]
+    if weights is None and Y.dtype is dt:
+        cfg = ec_sort_config(n, d, cfg.E, K, cfg.dtype, cfg.dtype)
     X_out = torch.empty(n, d, dtype=dt, device=dev) if X_out is None else X_out
     y, p, x = _dense("ec_combine", dev, (Y, _TYPES[cfg.y_dtype], (n * K, d)), (place, torch.int32, (n, K)), (X_out, dt, (n, d)))
     w = None if weights is None else _dense("ec_combine", dev, (weights, torch.float32, (n, K)))[0]

@@ -191,6 +191,26 @@ def test_gradient_of_the_dispatch():
         assert (X_s[:m].double() * C[:m].double()).sum() == (dX.double() * X.double()).sum()
 
 
+@pytest.mark.parametrize("dtype,y_dtype", [(F32, F32), (BF16, BF16), (BF16, F32)])
+def test_gradient_of_the_dispatch_in_each_pair_of_types(dtype, y_dtype):
+    """dX_s has X's type, whatever Y's is: the same identity in exact numbers, with the configuration of the layer, and the bits of a call
+    whose configuration has one type for both.  Rows of Y's type are still taken without weights."""
+    n, K, E, d = 90, 4, 9, 56
+    cfg = B.make_sort_config(n, d, E, K, dtype, y_dtype)
+    plan = B.ec_sort_tokens(cfg, _choice(n, K, E, 8, "holes").cuda())
+    g = torch.Generator(device="cuda").manual_seed(4)
+    X = torch.randint(-8, 9, (n, d), generator=g, device="cuda").to(dtype)
+    dX_s = torch.randint(-8, 9, (n * K, d), generator=g, device="cuda").to(dtype)
+    m = int(plan.offsets[-1])
+    X_s, dX = B.ec_dispatch(cfg, X, plan.place), B.ec_combine(cfg, dX_s, None, plan.place)
+    assert dX.dtype is dtype and (X_s[:m].double() * dX_s[:m].double()).sum() == (dX.double() * X.double()).sum()
+    assert torch.equal(dX, B.ec_combine(B.make_sort_config(n, d, E, K, dtype), dX_s, None, plan.place))
+    assert torch.equal(dX, B.ec_combine(cfg, dX_s.to(y_dtype), None, plan.place))
+    if y_dtype is not dtype:                              # with weights it is the layer's combine, and Y of its type
+        with pytest.raises(B.EcError):
+            B.ec_combine(cfg, dX_s, torch.ones(n, K, device="cuda"), plan.place)
+
+
 def _step(cfg, choice, X, Y, w, G, bufs, ws):
     plan = B.ec_sort_tokens(cfg, choice, out=bufs["plan"], ws=ws)
     B.ec_dispatch(cfg, X, plan.place, X_s=bufs["X_s"])
