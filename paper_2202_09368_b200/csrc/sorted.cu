@@ -159,7 +159,10 @@ __global__ void __launch_bounds__(kSortThreads) sort_rank_kernel(const SortArgs 
 #pragma unroll
     for (int u = 0; u < kHeld; ++u) put(i + 32 * u + lane, x[u], r[u]);
   }
-  if constexpr (HOW == ONE_CLUSTER) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if constexpr (HOW == ONE_CLUSTER) {
+    __syncwarp();                                     // the lanes took different ways through put(); .aligned wants the warp together
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
 }
 
 __global__ void __launch_bounds__(kSortThreads) sort_shift_kernel(const SortArgs a) {

@@ -54,6 +54,18 @@ def test_plan(n, K, E, kind):
     _check_plan(B.ec_sort_tokens(cfg, choice.cuda(), out=out), choice, E)
 
 
+@pytest.mark.parametrize("E", [3, 33, 256])
+def test_plans_of_a_cluster_whose_warps_end_unevenly(E):
+    """Totals that end inside a warp's round, with choices of no expert: lanes of a warp part before the cluster's last barrier."""
+    for total in (2049, 2063, 2080, 4097, 5003, 8191, 8193, 9999, 16383, 20011, 24575):
+        choice = _choice(total, 1, E, total, "holes")
+        cfg = B.make_sort_config(total, 64, E, 1)
+        on = choice.cuda()
+        for _ in range(5):
+            out = B.Sorted(*(torch.full(s, -77, dtype=torch.int32, device="cuda") for s in ((E + 1,), (total,), (total, 1))))
+            _check_plan(B.ec_sort_tokens(cfg, on, out=out), choice, E)
+
+
 # widths: below, at and beyond the lanes' stretches, odd numbers of 16-byte pieces, one piece
 WIDTHS = [(F32, F32, 4), (F32, F32, 36), (F32, F32, 1000), (BF16, BF16, 8), (BF16, BF16, 64), (BF16, BF16, 136), (BF16, BF16, 1000), (BF16, BF16, 4104),
           (BF16, F32, 8), (BF16, F32, 328), (BF16, F32, 2056), (F32, F32, 2052)]
