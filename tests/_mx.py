@@ -83,3 +83,18 @@ def check_product(got, z, size, K, dtype, kind="none"):
     bound = d + S.HALF_STEP[dtype] * (np.abs(want) + d) + S.TINY[dtype]
     inside = ~np.isnan(z)
     assert (err[inside] <= bound[inside]).all(), float((err - bound)[inside].max())
+
+
+def form(rows, N, K, E, sms, four_bits=False, gelu=False):
+    """How the product cuts its work: rows of a tile and its columns of C (clusters, which are for fewer tiles than CTAs, aside)."""
+    mean = rows // E
+    if mean <= 90:
+        return (32 if mean <= 2 else 64 if mean <= 20 else 128), 128
+    tiles, epilogue, stages = rows / 192 + 0.5 * E, 7000 if four_bits else 5200 if gelu else 2700, -(-K // 256)
+    rounds = lambda cols: math.ceil(tiles * -(-N // cols) / sms)
+    wide = rounds(256) * (stages * 1028 + 2 * epilogue + 1500) < rounds(128) * max(stages * 775 + 700, epilogue + 1100)
+    return 192, 256 if wide else 128
+
+
+def tiles(offsets, N, row_tile, columns):
+    return sum(-(-int(n) // row_tile) for n in np.diff(offsets)) * -(-N // columns)

@@ -6,6 +6,7 @@ import torch
 
 from paper_2202_09368_b200 import binding as B
 
+import _mx as M
 from test_gpu_debug_build import D  # noqa: F401  (the fixture: a second binding, of the debug library)
 
 pytestmark = pytest.mark.gpu
@@ -22,6 +23,25 @@ def _operands(M, rows, N, K, E):
 def test_a_product_whose_loads_never_come(D, rows, N, K, E):
     """One CTA loads nothing: the call ends, with the status of a wait that ran out, and the next one on the same workspace is as ever."""
     A, W, offsets = _operands(D, rows, N, K, E)
+    ws = torch.empty(D.EC_MX_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+    want = D.ec_mx_expert_gemm(A, W, offsets, ws=ws)
+    assert D.ec_read_status(ws) == D.EC_OK and torch.equal(want, B.ec_mx_expert_gemm(A, W, offsets))
+    cfg = D.ec_mx_gemm_config(rows, N, K, E, D.EC_MX_OUT_BF16, 0, 0)
+    call = D.lib().ec_debug_mx_wait
+    call.argtypes = [ctypes.POINTER(D.ec_mx_gemm_config)] + [ctypes.c_void_p] * 9 + [ctypes.c_size_t, ctypes.c_void_p]
+    out = torch.zeros_like(want)
+    assert call(ctypes.byref(cfg), A.codes.data_ptr(), A.scales.data_ptr(), offsets.data_ptr(), W.codes.data_ptr(), W.scales.data_ptr(), None,
+                out.data_ptr(), None, ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream) == D.EC_OK
+    assert D.ec_read_status(ws) == D.EC_ERR_TIMEOUT
+    assert torch.equal(D.ec_mx_expert_gemm(A, W, offsets, ws=ws), want) and D.ec_read_status(ws) == D.EC_OK
+
+
+@pytest.mark.parametrize("rows,N,K,E,columns", [(2400, 4096, 520, 8, 128), (4000, 8192, 4104, 8, 256)])
+def test_loads_that_never_come_where_a_cta_has_several_tiles(D, rows, N, K, E, columns):
+    """The same with three tiles and more to a CTA, in tiles of 128 and of 256 columns: the roles leave in the middle of their tiles."""
+    A, W, offsets = _operands(D, rows, N, K, E)
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert M.form(rows, N, K, E, sms) == (192, columns) and M.tiles(offsets.cpu(), N, 192, columns) > 2 * sms
     ws = torch.empty(D.EC_MX_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
     want = D.ec_mx_expert_gemm(A, W, offsets, ws=ws)
     assert D.ec_read_status(ws) == D.EC_OK and torch.equal(want, B.ec_mx_expert_gemm(A, W, offsets))
