@@ -77,3 +77,23 @@ def test_several_tiles_to_a_cta(rows, N, K, E, kind):
         assert torch.equal(q.codes[inside], same.codes[inside]) and torch.equal(q.scales[inside, :blocks], same.scales[inside, :blocks])
         for r in (slice(0, inside.start), slice(inside.stop, rows)):
             assert (q.codes[r] == 0xAA).all() and (q.scales[r] == 0xAA).all()
+
+
+@pytest.mark.parametrize("rows,N,K,E", [(256, 4096, 4104, 16), (480, 8192, 2056, 8), (2400, 4096, 520, 8), (4000, 8192, 4104, 8)])
+def test_the_same_bits_every_time(rows, N, K, E):
+    """Back to back, where a barrier passes a phase every few hundred cycles: no lane of the issuing warps misses one (it would wait for two
+    seconds and give up), and no result differs."""
+    g = torch.Generator(device="cuda").manual_seed(N)
+    A, W = _random((rows,), K, g), _random((E, N), K, g)
+    off = torch.from_numpy(_offsets(rows, E, 5)).int().cuda()
+    ws = torch.empty(B.EC_MX_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+    want = B.ec_mx_expert_gemm(A, W, off, out=torch.zeros(rows, N, device="cuda"), ws=ws)
+    assert B.ec_read_status(ws) == B.EC_OK
+    out = torch.zeros(rows, N, device="cuda")
+    wrong = torch.zeros((), dtype=torch.bool, device="cuda")
+    codes = torch.zeros((), dtype=torch.int32, device="cuda")
+    for _ in range(100):
+        B.ec_mx_expert_gemm(A, W, off, out=out, ws=ws)
+        codes |= ws[:4].view(torch.int32)[0]              # the status word of each call
+        wrong |= (out != want).any()
+    assert not wrong and codes == 0
