@@ -490,6 +490,7 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         const int col = walk.m * kTileM + h * kM + q * 32 + lane;
         const bool in = col < p.N;
         const float bias = biases[MT == 1 ? 0 : h];
+        __syncwarp();                                // the last chunk's stores parted the lanes
         uint32_t r[kChunk]; tc_ld16(taddr + h * NT + c, r);
         float v[kChunk];
 #pragma unroll
