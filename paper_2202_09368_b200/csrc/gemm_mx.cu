@@ -266,7 +266,8 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   const uint32_t tmem_base = *tmem_slot, smem_base = smem_u32(smem), scale_base = smem_base + S * kStage;
   // The first CTA clears the status word; another writes it two seconds into a wait at the earliest.
   if (blockIdx.x == 0 && threadIdx.x == 0) { p.status[0] = 0; p.status[1] = 0; }
-  // The groups: offsets are the caller's memory, whatever they hold becomes rows inside [0, rows).
+  // The groups: offsets are the caller's memory, whatever they hold becomes rows inside [0, rows) that no two groups share, so there are
+  // no more tiles than the host counted and a row has one writer.
   if (warp == 0) {
     const int32_t* offsets = after_enter(p.offsets);
     int from[kMaxE / 32], to[kMaxE / 32], active = 0, total = 0;
@@ -276,10 +277,26 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       from[i] = e < p.E ? __ldg(offsets + e) : 0;
       to[i] = e < p.E ? __ldg(offsets + e + 1) : 0;
     }
+    bool falls = false;
+#pragma unroll
+    for (int i = 0; i < kMaxE / 32; ++i) {
+      from[i] = min(max(from[i], 0), (int)p.rows); to[i] = min(max(to[i], 0), (int)p.rows);
+      falls |= to[i] < from[i];
+    }
+    if (__any_sync(0xffffffffu, falls)) {            // an offset counts as the largest up to it
+      int most = 0;
+#pragma unroll
+      for (int i = 0; i < kMaxE / 32; ++i) {
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) { const int v = __shfl_up_sync(0xffffffffu, from[i], o); if (lane >= o) from[i] = max(from[i], v); }
+        from[i] = max(from[i], most); to[i] = max(to[i], from[i]);
+        most = __shfl_sync(0xffffffffu, to[i], 31);
+      }
+    }
 #pragma unroll
     for (int i = 0; i < kMaxE / 32; ++i) {
       if (32 * i >= p.E) break;
-      const int e = 32 * i + lane, lo = (int)min((int64_t)max(from[i], 0), p.rows), count = max((int)min((int64_t)max(to[i], 0), p.rows) - lo, 0);
+      const int e = 32 * i + lane, lo = from[i], count = to[i] - lo;
       const unsigned some = __ballot_sync(0xffffffffu, count > 0);
       const int tiles = (count + NT - 1) / NT;
       int before = tiles;                            // of the lanes up to this one

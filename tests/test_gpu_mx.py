@@ -261,6 +261,28 @@ def test_offsets_are_cut_to_the_rows():
     assert lo[0] == 0 and lo[-1] == rows
 
 
+@pytest.mark.parametrize("rows,N,K,E", [(150, 136, 64, 6), (3, 72, 2048, 40), (700, 264, 96, 33), (900, 384, 512, 256), (2000, 512, 72, 5)])
+def test_groups_never_share_rows(rows, N, K, E):
+    """Offsets that fall count as the largest before them: the bits, in every row and every time, of a call with the rising offsets; rows of
+    no expert and what lies around C as they were."""
+    A, W, _, _ = _case(rows, N, K, E, 21)
+    g = np.random.default_rng(E)
+    tries = [np.array([0] + [rows, 0] * E)[: E + 1], np.array([rows, 0] * E)[: E + 1], np.array([5, -3] + [rows // 2, 1, 2 ** 31 - 1, -2 ** 31] * E)[: E + 1]]
+    tries += [g.integers(-5, rows + 5, E + 1) for _ in range(5)]
+    for offsets in tries:
+        rising = np.maximum.accumulate(np.clip(offsets, 0, rows))
+
+        def run(o):
+            around = torch.full((rows + 2, N), 7.0, device="cuda")
+            B.ec_mx_expert_gemm(A, W, torch.from_numpy(o).int().cuda(), dtype=F32, out=around[1:-1])
+            return around
+
+        want, got = run(rising), run(offsets)
+        assert torch.equal(got, want)
+        assert (got[: 1 + rising[0]] == 7.0).all() and (got[1 + rising[-1]:] == 7.0).all()
+        assert rising[0] == rising[-1] or not (got[1 + rising[0]: 1 + rising[-1]] == 7.0).all(1).any()
+
+
 def _layer(n, K, E, d, f, act, seed):
     g = torch.Generator().manual_seed(seed)
     data = dict(choice=torch.randint(-1, E, (n, K), generator=g, dtype=torch.int32).cuda(), X=torch.randn(n, d, generator=g).to(BF16).cuda(),
