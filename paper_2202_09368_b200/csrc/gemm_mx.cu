@@ -171,7 +171,8 @@ __device__ __forceinline__ void tc_st_wait() { asm volatile("tcgen05.wait::st.sy
 
 // GeLU of a pair, z Phi(z).  erf(u) = u Q(t) with t = 2 u^2 / U^2 - 1, U = 3.8 (erf(3.8) = 1 - 8e-8), Q the degree-14 polynomial through the
 // Chebyshev nodes in t of erf(u) / u (fitted for this file; coefficients of the powers of t, all below 1/2, so Horner's rule is stable).
-// |error| < 2.6e-7 |z| in fp32, a third of the instructions of erff; below -U sqrt 2 z counts as that, NaN stays NaN.
+// |error| < 2.6e-7 |z| in fp32, a third of the instructions of erff; below -U sqrt 2 z counts as that, NaN stays NaN.  Phi is held in [0, 1]
+// (by the instruction that adds its half), so that in the tail, where the error is as large as the value, the sign is still z's.
 __device__ __forceinline__ void gelu_erf2(float& z0, float& z1) {
   constexpr float U = 3.8f, Z = -5.374011538f;
   asm("max.NaN.f32 %0, %0, %1;" : "+f"(z0) : "f"(Z)); asm("max.NaN.f32 %0, %0, %1;" : "+f"(z1) : "f"(Z));
@@ -184,7 +185,8 @@ __device__ __forceinline__ void gelu_erf2(float& z0, float& z1) {
   unsigned long long acc = pk2(c[14], c[14]);
 #pragma unroll
   for (int i = 13; i >= 0; --i) acc = fma2(acc, t, pk2(c[i], c[i]));
-  const unsigned long long h = mul2(z, fma2(mul2(uc, acc), pk2(0.5f, 0.5f), pk2(0.5f, 0.5f)));
+  const unsigned long long erf = mul2(uc, acc);
+  const unsigned long long h = mul2(z, pk2(__saturatef(fmaf(lo2(erf), 0.5f, 0.5f)), __saturatef(fmaf(hi2(erf), 0.5f, 0.5f))));
   z0 = lo2(h); z1 = hi2(h);
 }
 
