@@ -385,7 +385,8 @@ typedef struct {
  * most 2.6e-7 |z|, which is a part in a thousand of its value at z = -4 and most of it below -5, and has z's sign or is zero.
  * Rows of no expert are left as they were.  Any contents of `offsets` are safe to pass: they are cut to [0, rows], and one that falls
  * counts as the largest before it, so groups never share rows.
- * rows = 0: nothing to do.  `ws`: 256 bytes, 256-byte aligned, for the status word (ec_read_status).
+ * rows = 0: nothing to do.  `ws`: 256 bytes, 256-byte aligned, for the status word.  Where ec_read_status answers that a wait ran
+ * out, C is undefined, and so is what later products made of it.
  */
 #define EC_MX_WORKSPACE_BYTES 256
 ec_status ec_mx_expert_gemm(const ec_mx_gemm_config* cfg, const uint8_t* A, const uint8_t* A_scales, const int32_t* offsets,
@@ -415,8 +416,10 @@ ec_status ec_backward_view(const ec_config* cfg, void* ws, ec_backward_ptrs* out
  * on `ws` left there: EC_OK, or EC_ERR_TIMEOUT when a bounded wait inside a kernel
  * gave up (the outputs of that call are then undefined), or EC_ERR_INDEX (debug build)
  * when an index was out of range, or EC_ERR_CUDA when the stream reports an error.
+ * ec_mx_expert_gemm leaves the EC_ERR_TIMEOUT of an earlier ec_mx_expert_gemm on the workspace in the word, so that
+ * one read answers for a chain of them; the read that reports it clears it.  Every other call starts the word anew.
  */
-ec_status ec_read_status(const void* ws, void* cuda_stream);
+ec_status ec_read_status(void* ws, void* cuda_stream);
 
 /* Static, NUL-terminated description of a status code. */
 const char* ec_status_string(ec_status s);

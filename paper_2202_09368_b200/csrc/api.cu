@@ -663,11 +663,14 @@ int ec_debug_build(void) {
 #endif
 }
 
-ec_status ec_read_status(const void* ws, void* stream) {
+ec_status ec_read_status(void* ws, void* stream) {
   if (!ws) return EC_ERR_INVALID_ARG;
   StatusWord h;
   if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return EC_ERR_CUDA;
   if (cudaMemcpy(&h, ws, sizeof(h), cudaMemcpyDeviceToHost) != cudaSuccess) return EC_ERR_CUDA;
+  if (h.code == EC_ERR_TIMEOUT && (h.where & kStatusMark) == kStatusStays) {      // it has stayed for this call
+    if (cudaMemsetAsync(ws, 0, 8, (cudaStream_t)stream) != cudaSuccess || cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return EC_ERR_CUDA;
+  }
   return h.code == 0 ? EC_OK : (h.code == EC_ERR_TIMEOUT ? EC_ERR_TIMEOUT : (h.code == EC_ERR_INDEX ? EC_ERR_INDEX : EC_ERR_CUDA));
 }
 

@@ -96,7 +96,7 @@ __device__ __forceinline__ uint32_t elect_one() {
 // the barrier pass through the phase that a slower lane still waits for.  (32768 rows, 4096 x 16384: 1443 us with and without the
 // __syncwarp(), 1451 with votes on what the lanes have seen.)
 __device__ __forceinline__ void wait(uint32_t& alive, uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int where) {
-  if (alive && !mbar_try(bar, parity)) alive = mbar_wait(bar, parity, abort_flag, status, where);
+  if (alive && !mbar_try(bar, parity)) alive = mbar_wait(bar, parity, abort_flag, status, kStatusStays | where);
   __syncwarp();
 }
 __device__ __forceinline__ void expect_tx_if(uint32_t lead, uint32_t bar, uint32_t bytes) {
@@ -141,7 +141,7 @@ __device__ __forceinline__ bool cluster_wait(uint32_t bar, uint32_t parity, vola
         if (*abort_flag) { ok = false; break; }
         if (globaltimer() - t0 > kWaitNs) {
           *abort_flag = 1;
-          atomicExch(status + 1, where); atomicExch(status, EC_ERR_TIMEOUT);
+          atomicExch(status + 1, kStatusStays | where); atomicExch(status, EC_ERR_TIMEOUT);
           ok = false;
           break;
         }
@@ -158,7 +158,7 @@ __device__ __forceinline__ void st_cluster4(uint32_t addr, const float* v) {
 // A warp's wait with an answer: one lane polls.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int where, int lane) {
   bool ok = true;
-  if (lane == 0) ok = mbar_wait(bar, parity, abort_flag, status, where);
+  if (lane == 0) ok = mbar_wait(bar, parity, abort_flag, status, kStatusStays | where);
   ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
   __syncwarp();                                      // what the lane has seen the others see
   return ok;
@@ -267,7 +267,7 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   chain_enter();
   const uint32_t tmem_base = *tmem_slot, smem_base = smem_u32(smem), scale_base = smem_base + S * kStage;
   // The first CTA clears the status word; another writes it two seconds into a wait at the earliest.
-  if (blockIdx.x == 0 && threadIdx.x == 0) { p.status[0] = 0; p.status[1] = 0; }
+  if (blockIdx.x == 0 && threadIdx.x == 0) begin_status(p.status);
   // The groups: offsets are the caller's memory, whatever they hold becomes rows inside [0, rows) that no two groups share, so there are
   // no more tiles than the host counted and a row has one writer.
   if (warp == 0) {
@@ -316,7 +316,7 @@ gemm_mx_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   __syncthreads();
   const int total = __shfl_sync(0xffffffffu, groups->total, 0);
   bool gave_up = tmem_base != 0;                     // cannot happen with all 512 columns taken; refuse rather than corrupt
-  if (gave_up && threadIdx.x == 0) { atomicExch(p.status + 1, 9); atomicExch(p.status, EC_ERR_TIMEOUT); }
+  if (gave_up && threadIdx.x == 0) { atomicExch(p.status + 1, kStatusStays | 9); atomicExch(p.status, EC_ERR_TIMEOUT); }
 
   if (gave_up) {
     // nothing: fall through to the exit

@@ -20,6 +20,13 @@ constexpr int kSortTile = 4096;    // 64-bit keys sorted in shared memory by one
 // I, row_ptr or slots was out of range); word 2 counts such indices.
 struct StatusWord { int code; int where; int bad_indices; int pad[61]; };
 constexpr int kStatusWords = sizeof(StatusWord) / 4;
+// A 4-bit product's wait that ran out is marked in `where`: later products and plans on the same workspace then leave the word as it is
+// (each product of a chain may have one workspace) until ec_read_status has reported it.
+constexpr int kStatusStays = 0x4D580000, kStatusMark = 0x7FFF0000;
+__device__ __forceinline__ void begin_status(int* status) {
+  volatile int* s = status;
+  if (s[0] != 5 || (s[1] & kStatusMark) != kStatusStays) { s[0] = 0; s[1] = 0; }
+}
 constexpr int kSelectCounter = 16;                   // word of the status block: CTAs of the selection that are done
 
 // Debug build (-DEC_DEBUG): every index read from I, row_ptr or slots is checked against its range before it is used;

@@ -53,3 +53,34 @@ def test_loads_that_never_come_where_a_cta_has_several_tiles(D, rows, N, K, E, c
                 out.data_ptr(), None, ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream) == D.EC_OK
     assert D.ec_read_status(ws) == D.EC_ERR_TIMEOUT
     assert torch.equal(D.ec_mx_expert_gemm(A, W, offsets, ws=ws), want) and D.ec_read_status(ws) == D.EC_OK
+
+
+def _silent(D, cfg, A, W, offsets, out, ws):
+    """A product whose first CTA loads nothing."""
+    call = D.lib().ec_debug_mx_wait
+    call.argtypes = [ctypes.POINTER(D.ec_mx_gemm_config)] + [ctypes.c_void_p] * 9 + [ctypes.c_size_t, ctypes.c_void_p]
+    assert call(ctypes.byref(cfg), A.codes.data_ptr(), A.scales.data_ptr(), offsets.data_ptr(), W.codes.data_ptr(), W.scales.data_ptr(), None,
+                out.data_ptr(), None, ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream) == D.EC_OK
+
+
+@pytest.mark.parametrize("rows,N,K,E", [(1, 128, 8192, 1), (64, 256, 512, 2), (900, 384, 512, 2)])
+def test_a_wait_that_ran_out_is_not_lost_behind_a_later_product(D, rows, N, K, E):
+    """A chain of products on one workspace is asked once, at its end; the answer is given once, and a call of another kind starts anew."""
+    A, W, offsets = _operands(D, rows, N, K, E)
+    for fill in (0, 0xA5, 5):                             # whatever the workspace holds before its first use
+        ws = torch.full((D.EC_MX_WORKSPACE_BYTES,), fill, dtype=torch.uint8, device="cuda")
+        want = D.ec_mx_expert_gemm(A, W, offsets, ws=ws)
+        assert D.ec_read_status(ws) == D.EC_OK
+    cfg = D.ec_mx_gemm_config(rows, N, K, E, D.EC_MX_OUT_BF16, 0, 0)
+    _silent(D, cfg, A, W, offsets, torch.zeros_like(want), ws)
+    for _ in range(3):
+        assert torch.equal(D.ec_mx_expert_gemm(A, W, offsets, ws=ws), want)
+    assert D.ec_read_status(ws) == D.EC_ERR_TIMEOUT
+    assert D.ec_read_status(ws) == D.EC_OK
+    assert torch.equal(D.ec_mx_expert_gemm(A, W, offsets, ws=ws), want) and D.ec_read_status(ws) == D.EC_OK
+    layer = D.make_config(256, 64, 128, 4, 2.0, torch.bfloat16)
+    ws = D.alloc_workspace(layer)
+    _silent(D, cfg, A, W, offsets, torch.zeros_like(want), ws)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    D.ec_route(layer, *(torch.empty(s, device="cuda").normal_(generator=g).to(torch.bfloat16) for s in ((256, 64), (64, 4))), ws=ws)
+    assert D.ec_read_status(ws) == D.EC_OK
