@@ -416,8 +416,9 @@ ec_status ec_backward_view(const ec_config* cfg, void* ws, ec_backward_ptrs* out
  * on `ws` left there: EC_OK, or EC_ERR_TIMEOUT when a bounded wait inside a kernel
  * gave up (the outputs of that call are then undefined), or EC_ERR_INDEX (debug build)
  * when an index was out of range, or EC_ERR_CUDA when the stream reports an error.
- * ec_mx_expert_gemm leaves the EC_ERR_TIMEOUT of an earlier ec_mx_expert_gemm on the workspace in the word, so that
- * one read answers for a chain of them; the read that reports it clears it.  Every other call starts the word anew.
+ * ec_mx_expert_gemm and ec_sort_tokens leave the EC_ERR_TIMEOUT of an earlier ec_mx_expert_gemm on the workspace in
+ * the word, so that one read answers for a chain of them; the read that reports it clears it.  Every other call
+ * starts the word anew.
  */
 ec_status ec_read_status(void* ws, void* cuda_stream);
 

@@ -181,7 +181,7 @@ cudaError_t launch_gather_gate(const float* S, const int32_t* I, float* G, int64
                                int64_t n, int* status, cudaStream_t st);
 
 // ---- tokens sorted by expert (sorted.cu) ---------------------------------------------------------
-// total = n * per_token flat choices; scratch as sort_scratch_bytes says
+// total = n * per_token flat choices; scratch as sort_scratch_bytes says, the status block first
 size_t sort_scratch_bytes(int E);
 cudaError_t launch_sort_tokens(const int32_t* choice, int64_t total, int E, int32_t* offsets, int32_t* order, int32_t* place,
                                void* scratch, cudaStream_t st);

@@ -26,7 +26,7 @@ constexpr int kHeld = 4;                              // rounds of 32 choices wh
 enum { ONE_CTA, ONE_CLUSTER, TWO_LAUNCHES };
 
 struct SortArgs {
-  const int32_t* choice; int32_t* offsets; int32_t* order; int32_t* place; int* counts;   // counts [pieces, E]
+  const int32_t* choice; int32_t* offsets; int32_t* order; int32_t* place; int* status; int* counts;   // counts [pieces, E]
   int64_t total, per_cta;                                                                  // flat choices; per_cta a multiple of 1024
   int E, bits, pieces;                                                                     // bits: of an expert's number
 };
@@ -68,6 +68,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_rank_kernel(const SortArgs 
   for (int e = lane; e < E; e += 32) counters[warp][e] = 0;
   __syncwarp();
   chain_enter();
+  if (blockIdx.x == 0 && threadIdx.x == kSortThreads - 1) begin_status(a.status);
   const int32_t* choice = after_enter(a.choice);
   const int64_t per_warp = a.per_cta / kSortWarps, lo = blockIdx.x * a.per_cta + warp * per_warp, hi = min(lo + per_warp, a.total);
   int* mine = counters[warp];
@@ -467,10 +468,10 @@ cudaError_t backward_of(const void* dX_out, const void* Y, const float* w, const
 
 }  // namespace
 
-size_t sort_scratch_bytes(int E) { return (size_t)kMaxPieces * E * 4; }
+size_t sort_scratch_bytes(int E) { return sizeof(StatusWord) + (size_t)kMaxPieces * E * 4; }
 
 cudaError_t launch_sort_tokens(const int32_t* choice, int64_t total, int E, int32_t* offsets, int32_t* order, int32_t* place, void* scratch, cudaStream_t st) {
-  SortArgs a{choice, offsets, order, place, (int*)scratch, total, 0, E, 0, 1};
+  SortArgs a{choice, offsets, order, place, (int*)scratch, (int*)((char*)scratch + sizeof(StatusWord)), total, 0, E, 0, 1};
   while ((1 << a.bits) < E) ++a.bits;
   auto cut = [&](int ctas) { a.per_cta = ((total + ctas - 1) / ctas + 1023) / 1024 * 1024; };
   if (total <= kOnePiece) {

@@ -84,3 +84,15 @@ def test_a_wait_that_ran_out_is_not_lost_behind_a_later_product(D, rows, N, K, E
     g = torch.Generator(device="cuda").manual_seed(1)
     D.ec_route(layer, *(torch.empty(s, device="cuda").normal_(generator=g).to(torch.bfloat16) for s in ((256, 64), (64, 4))), ws=ws)
     assert D.ec_read_status(ws) == D.EC_OK
+
+
+@pytest.mark.parametrize("n", [3, 3000, 20000])
+def test_nor_behind_a_plan(D, n):
+    """Nor do a plan's counts land in the word: in one CTA, in a cluster and in two launches."""
+    A, W, offsets = _operands(D, 64, 256, 512, 2)
+    sort = D.make_sort_config(n, 64, 200, 2)
+    choice = torch.randint(0, 200, (n, 2), generator=torch.Generator().manual_seed(n), dtype=torch.int32).cuda()
+    ws = torch.empty(D.ec_sort_workspace_bytes(sort), dtype=torch.uint8, device="cuda")
+    _silent(D, D.ec_mx_gemm_config(64, 256, 512, 2, D.EC_MX_OUT_BF16, 0, 0), A, W, offsets, torch.zeros(64, 256, dtype=torch.bfloat16, device="cuda"), ws)
+    D.ec_sort_tokens(sort, choice, ws=ws)
+    assert D.ec_read_status(ws) == D.EC_ERR_TIMEOUT

@@ -66,6 +66,19 @@ def test_plans_of_a_cluster_whose_warps_end_unevenly(E):
             _check_plan(B.ec_sort_tokens(cfg, on, out=out), choice, E)
 
 
+@pytest.mark.parametrize("n,E", [(7, 8), (5000, 8), (40000, 8), (30000, 256)])
+def test_status_of_a_plan(n, E):
+    """The plan's scratch begins with the status word, as every workspace does: nothing of its own lands there, whatever the memory held."""
+    cfg = B.make_sort_config(n, 64, E, 1)
+    choice = torch.full((n, 1), 5, dtype=torch.int32)
+    choice[: n // 2] = 0
+    for fill in (0, 0xA5, 5):
+        ws = torch.full((B.ec_sort_workspace_bytes(cfg) + 256,), fill, dtype=torch.uint8, device="cuda")
+        out = B.Sorted(*(torch.full(s, -77, dtype=torch.int32, device="cuda") for s in ((E + 1,), (n,), (n, 1))))
+        _check_plan(B.ec_sort_tokens(cfg, choice.cuda(), out=out, ws=ws[:-256]), choice, E)
+        assert B.ec_read_status(ws) == B.EC_OK and (ws[-256:] == fill).all()
+
+
 # widths: below, at and beyond the lanes' stretches, odd numbers of 16-byte pieces, one piece
 WIDTHS = [(F32, F32, 4), (F32, F32, 36), (F32, F32, 1000), (BF16, BF16, 8), (BF16, BF16, 64), (BF16, BF16, 136), (BF16, BF16, 1000), (BF16, BF16, 4104),
           (BF16, F32, 8), (BF16, F32, 328), (BF16, F32, 2056), (F32, F32, 2052)]
