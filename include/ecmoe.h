@@ -296,6 +296,7 @@ ec_status ec_validate_routing(const ec_config* cfg, const int32_t* I, const int3
  *   order   [n * per_token] int32, row r < m holds flat choice order[r] = t * per_token + j (token t), ascending inside an expert;
  *                           entries from m on are left as they were
  *   place   [n, per_token]  int32, the row of each choice, -1 where it names no expert: the inverse of `order`
+ * These four may begin at any multiple of 4 bytes (a slice of the tokens, one layer of a stack); everything else at 16.
  * Row matrices (X_s, Y, dY) have n * per_token rows, of which the first m are read and written; the others are left as they were.
  * X, X_out, dX_out and X_s have the element type cfg->dtype, Y and dY cfg->y_dtype, weights and dweights are fp32.
  * Restrictions (EC_ERR_UNSUPPORTED): rows of d_model elements of either type a multiple of 16 bytes, d_model <= 2^22 - 64,
@@ -378,8 +379,8 @@ typedef struct {
 
 /*
  * C[r, :] = act(A[r, :] . B[e]^T + bias[e, :]) for the rows offsets[e] <= r < offsets[e + 1] of expert e: groups of any length,
- * also none.  A [rows, K] and B [E, N, K] in the format above, offsets [E + 1] as ec_sort_tokens writes them (or i * k for the slots
- * of expert choice), bias [E, N] or NULL; C [rows, N] fp32 or bf16, dense, or the codes of the result as blocks along N with its scales
+ * also none.  A [rows, K] and B [E, N, K] in the format above, offsets [E + 1] (at any multiple of 4 bytes) as ec_sort_tokens writes them (or i * k
+ * for the slots of expert choice), bias [E, N] or NULL; C [rows, N] fp32 or bf16, dense, or the codes of the result as blocks along N with its scales
  * in C_scales (NULL otherwise), ready to be the next product's A.  Products are exact, sums fp32 (in an order that depends on the call's
  * sizes alone; what is below fp32's normal range may count as zero), bias and act fp32, one rounding.  The erf form of GeLU is off by at
  * most 2.6e-7 |z|, which is a part in a thousand of its value at z = -4 and most of it below -5, and has z's sign or is zero.

@@ -10,6 +10,8 @@ inline bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)
 inline size_t esize(int dtype) { return dtype == EC_F32 ? 4 : 2; }
 inline bool overlap(const void* a, size_t na, const void* b, size_t nb) { return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na; }
 template <typename... P> bool bad_pointers(P... p) { return ((p == nullptr || misaligned(p, 16)) || ...); }
+// choice, offsets, order and place are read and written one by one: a slice of rows, or one layer of a stack, need not begin at 16 bytes
+template <typename... P> bool bad_indices(const P*... p) { return ((p == nullptr || misaligned(p, 4)) || ...); }
 
 #define EC_CUDA(x) do { if ((x) != cudaSuccess) return EC_ERR_CUDA; } while (0)
 
@@ -32,8 +34,8 @@ ec_status ec_sort_tokens(const ec_sort_config* c, const int32_t* choice, int32_t
                          void* stream) {
   const ec_status s = check_sort(c);
   if (s != EC_OK) return s;
-  if (bad_pointers(offsets) || ws == nullptr || misaligned(ws, 256)) return EC_ERR_INVALID_ARG;
-  if (c->n > 0 && bad_pointers(choice, order, place)) return EC_ERR_INVALID_ARG;
+  if (bad_indices(offsets) || ws == nullptr || misaligned(ws, 256)) return EC_ERR_INVALID_ARG;
+  if (c->n > 0 && bad_indices(choice, order, place)) return EC_ERR_INVALID_ARG;
   if (ws_bytes < ec_sort_workspace_bytes(c)) return EC_ERR_WORKSPACE;
   if (c->n > 0) {      // the kernels index by what they read back of these arrays
     const size_t flat = (size_t)(c->n * c->per_token) * 4;
@@ -49,7 +51,7 @@ ec_status ec_sort_tokens(const ec_sort_config* c, const int32_t* choice, int32_t
 ec_status ec_dispatch(const ec_sort_config* c, const void* X, const int32_t* place, void* X_s, void* stream) {
   const ec_status s = check_sort(c);
   if (s != EC_OK || c->n == 0) return s;
-  if (bad_pointers(X, place, X_s)) return EC_ERR_INVALID_ARG;
+  if (bad_pointers(X, X_s) || bad_indices(place)) return EC_ERR_INVALID_ARG;
   EC_CUDA(launch_dispatch(X, place, X_s, c->n, c->d_model * (int64_t)esize(c->dtype), c->per_token, (cudaStream_t)stream));
   return EC_OK;
 }
@@ -57,7 +59,7 @@ ec_status ec_dispatch(const ec_sort_config* c, const void* X, const int32_t* pla
 ec_status ec_combine(const ec_sort_config* c, const void* Y, const float* weights, const int32_t* place, void* X_out, void* stream) {
   const ec_status s = check_sort(c);
   if (s != EC_OK || c->n == 0) return s;
-  if (bad_pointers(Y, place, X_out) || (weights != nullptr && misaligned(weights, 16))) return EC_ERR_INVALID_ARG;
+  if (bad_pointers(Y, X_out) || bad_indices(place) || (weights != nullptr && misaligned(weights, 16))) return EC_ERR_INVALID_ARG;
   EC_CUDA(launch_combine_rows(c->dtype, c->y_dtype, Y, weights, place, X_out, c->n, c->d_model, c->per_token, (cudaStream_t)stream));
   return EC_OK;
 }
@@ -66,7 +68,7 @@ ec_status ec_combine_backward(const ec_sort_config* c, const void* dX_out, const
                               float* dweights, void* stream) {
   const ec_status s = check_sort(c);
   if (s != EC_OK || c->n == 0) return s;
-  if (bad_pointers(dX_out, Y, weights, place, dY, dweights)) return EC_ERR_INVALID_ARG;
+  if (bad_pointers(dX_out, Y, weights, dY, dweights) || bad_indices(place)) return EC_ERR_INVALID_ARG;
   EC_CUDA(launch_combine_backward(c->dtype, c->y_dtype, dX_out, Y, weights, place, dY, dweights, c->n, c->d_model, c->per_token, (cudaStream_t)stream));
   return EC_OK;
 }
@@ -102,7 +104,7 @@ ec_status ec_mx_dequantize(int dtype, const uint8_t* codes, const uint8_t* scale
 ec_status ec_mx_dispatch(const ec_sort_config* c, const void* X, const int32_t* place, uint8_t* codes, uint8_t* scales, void* stream) {
   const ec_status s = check_sort(c);
   if (s != EC_OK || c->n == 0) return s;
-  if (bad_pointers(X, place, codes, scales)) return EC_ERR_INVALID_ARG;
+  if (bad_pointers(X, codes, scales) || bad_indices(place)) return EC_ERR_INVALID_ARG;
   EC_CUDA(launch_mx_dispatch(c->dtype, X, place, c->n, c->d_model, c->per_token, codes, scales, (cudaStream_t)stream));
   return EC_OK;
 }
@@ -118,7 +120,7 @@ static ec_status mx_expert_gemm(const ec_mx_gemm_config* c, const uint8_t* A, co
   if (ws == nullptr || misaligned(ws, 256)) return EC_ERR_INVALID_ARG;
   if (ws_bytes < EC_MX_WORKSPACE_BYTES) return EC_ERR_WORKSPACE;
   if (c->rows == 0) return EC_OK;
-  if (bad_pointers(A, A_scales, offsets, B, B_scales, C) || (bias != nullptr && misaligned(bias, 16))) return EC_ERR_INVALID_ARG;
+  if (bad_pointers(A, A_scales, B, B_scales, C) || bad_indices(offsets) || (bias != nullptr && misaligned(bias, 16))) return EC_ERR_INVALID_ARG;
   if (c->out == EC_MX_OUT_MX ? bad_pointers(C_scales) : C_scales != nullptr) return EC_ERR_INVALID_ARG;
   MxGemmArgs g{c->rows, c->N, c->K, c->E, c->out, c->act, A, A_scales, offsets, B, B_scales, bias, c->bias_dtype, C, C_scales, (int*)ws, silent};
   EC_CUDA(launch_gemm_mx(g, (cudaStream_t)stream));

@@ -236,6 +236,37 @@ def test_gradient_of_the_dispatch_in_each_pair_of_types(dtype, y_dtype):
             B.ec_combine(cfg, dX_s, torch.ones(n, K, device="cuda"), plan.place)
 
 
+@pytest.mark.parametrize("n,K,E,first", [(50, 3, 10, 1), (3000, 3, 10, 7), (30000, 1, 33, 3)])
+def test_slices_of_the_tokens_and_of_a_stack(n, K, E, first):
+    """choice[t0:] of an odd number of choices, a plan written into the middle of larger arrays, one layer's offsets of a stack: the results of
+    arrays of their own."""
+    d, dtype = 72, BF16
+    choice = _choice(first + n, K, E, 5, "holes").cuda()[first:]
+    assert choice.data_ptr() % 16
+    cfg = B.make_sort_config(n, d, E, K, dtype)
+    want = B.ec_sort_tokens(cfg, choice.clone())
+    stack = torch.full((3, E + 1), -77, dtype=torch.int32, device="cuda")
+    order, place = (torch.full((n * K + 2,), -77, dtype=torch.int32, device="cuda") for _ in range(2))
+    got = B.ec_sort_tokens(cfg, choice, out=B.Sorted(stack[1], order[1:-1], place[1:-1].view(n, K)))
+    m = int(want.offsets[-1])
+    assert torch.equal(got.offsets, want.offsets) and torch.equal(got.place, want.place) and torch.equal(got.order[:m], want.order[:m])
+    assert (stack[::2] == -77).all() and all((t[[0, -1]] == -77).all() for t in (order, place))
+    g = torch.Generator(device="cuda").manual_seed(2)
+    X, Y, G, w = (torch.randn(s, generator=g, device="cuda").to(t) for s, t in (((n, d), dtype), ((n * K, d), dtype), ((n, d), dtype), ((n, K), F32)))
+    calls = (lambda p: [B.ec_dispatch(cfg, X, p, X_s=torch.zeros_like(Y))], lambda p: [B.ec_combine(cfg, Y, w, p)],
+             lambda p: B.ec_combine_backward(cfg, G, Y, w, p, dY=torch.zeros_like(Y)))
+    for call in calls:
+        for a, b in zip(call(got.place), call(want.place)):
+            assert torch.equal(a, b)
+    zero = lambda: B.Mx(*(torch.zeros_like(t) for t in (q.codes, q.scales)), d)
+    q = B.alloc_mx((n * K, d))
+    a, b = (B.ec_mx_dispatch(cfg, X, p.place, out=zero()) for p in (got, want))
+    assert torch.equal(a.codes, b.codes) and torch.equal(a.scales, b.scales)
+    W = B.ec_mx_quantize(torch.randn(E, 64, d, generator=g, device="cuda"))
+    out = [B.ec_mx_expert_gemm(a, W, p.offsets, out=torch.zeros(n * K, 64, device="cuda")) for p in (got, want)]
+    assert torch.equal(*out)
+
+
 def _step(cfg, choice, X, Y, w, G, bufs, ws):
     plan = B.ec_sort_tokens(cfg, choice, out=bufs["plan"], ws=ws)
     B.ec_dispatch(cfg, X, plan.place, X_s=bufs["X_s"])

@@ -58,6 +58,23 @@ def test_pointers():
         assert f(None) == 0
 
 
+@pytest.mark.parametrize("at", [4097, 4098, 4102])
+def test_indices_that_are_not_whole_words(at):
+    """choice, offsets, order and place need 4 bytes' alignment, and that they need."""
+    cfg, L, p = B.make_sort_config(16, 64, 8, 2), B.lib(), [i << 20 for i in range(1, 8)]
+    r = C.byref(cfg)
+    for i in range(4):
+        args = p[:4]
+        args[i] += at - 4096
+        assert L.ec_sort_tokens(r, *args, 16 << 20, 1 << 18, None) == B.EC_ERR_INVALID_ARG
+    assert L.ec_dispatch(r, p[0], at, p[1], None) == B.EC_ERR_INVALID_ARG
+    assert L.ec_combine(r, p[0], None, at, p[1], None) == B.EC_ERR_INVALID_ARG
+    assert L.ec_combine_backward(r, p[0], p[1], p[2], at, p[3], p[4], None) == B.EC_ERR_INVALID_ARG
+    assert L.ec_mx_dispatch(r, p[0], at, p[1], p[2], None) == B.EC_ERR_INVALID_ARG
+    gemm = B.ec_mx_gemm_config(16, 64, 64, 2, B.EC_MX_OUT_BF16, 0, 0)
+    assert L.ec_mx_expert_gemm(C.byref(gemm), p[0], p[1], at, p[2], p[3], None, p[4], None, p[5], 256, None) == B.EC_ERR_INVALID_ARG
+
+
 @pytest.mark.parametrize("one,other", list(itertools.combinations(range(5), 2)))
 @pytest.mark.parametrize("shift", [0, 16])
 def test_arrays_of_the_plan_that_overlap(one, other, shift):
