@@ -120,6 +120,13 @@ def test_rows_there_and_back(dtype, y_dtype, d, n, K, E, kind):
     assert (dw.cpu().numpy()[place < 0] == 0).all()
 
 
+@pytest.mark.parametrize("dtype,y_dtype,d", [(BF16, BF16, 72), (BF16, BF16, 120), (BF16, BF16, 128), (BF16, F32, 40), (BF16, F32, 64), (F32, F32, 64)])
+@pytest.mark.parametrize("n,K,E,kind", [(1, 1, 4, "random"), (37, 1, 10, "holes"), (301, 2, 8, "holes"), (130, 3, 10, "holes"), (55, 4, 16, "random"), (19, 32, 256, "holes")])
+def test_rows_of_nine_to_sixteen_pieces(dtype, y_dtype, d, n, K, E, kind):
+    """Rows that two tokens of a warp share, by twos and by fours."""
+    test_rows_there_and_back(dtype, y_dtype, d, n, K, E, kind)
+
+
 def test_infinities_and_nan_stay_where_they_belong():
     """A row with NaN or an infinity reaches the tokens that hold it and no others, a weight of zero does not hide it (0 * inf is NaN),
     and what lies in rows without a choice reaches nobody."""
@@ -199,6 +206,52 @@ def test_gradients_against_differences(dtype):
         step = float(up[r, c].double() - down[r, c].double())
         t = int(plan.order[r]) // K
         assert abs((a - b) / step - float(dY[r, c])) <= (ea[t, c] + eb[t, c]) / step + 2.0 ** -23 * abs(float(dY[r, c])) + 1e-12
+
+
+@pytest.mark.parametrize("dtype,y_dtype", [(F32, F32), (BF16, F32), (BF16, BF16)])
+def test_gradients_against_differences_of_chosen_entries(dtype, y_dtype):
+    """As above with entries that are the same in every run: weights of choices that have a row (and one that has none, whose gradient is 0),
+    values of rows of every expert.  Y's steps of 4 from small multiples of 1/8 are exact in either type."""
+    n, K, E, d, h = 40, 3, 6, 48, 4.0
+    choice = _choice(n, K, E, 7, "holes")
+    cfg = B.make_sort_config(n, d, E, K, dtype, y_dtype)
+    plan = B.ec_sort_tokens(cfg, choice.cuda())
+    offsets, order, place = R.plan(choice.numpy(), E)
+    g = torch.Generator().manual_seed(11)
+    Y = (torch.randint(-16, 17, (n * K, d), generator=g) / 8).to(y_dtype).cuda()
+    w, C = torch.randn(n, K, generator=g).cuda(), torch.randn(n, d, generator=g).to(dtype).cuda()
+    dY, dw = B.ec_combine_backward(cfg, C, Y, w, plan.place, dY=torch.zeros_like(Y))
+    c = C.double().cpu().numpy()
+
+    def loss(Y, w):
+        out = B.ec_combine(cfg, Y, w, plan.place)
+        want, size = R.combine(Y, w, place)
+        sums = (2 * K + 2) * 2.0 ** -24 * size            # the fp32 sums' own error, and the rounding of what they came to
+        return c * out.double().cpu().numpy(), (sums + R.HALF_STEP[dtype] * (np.abs(want) + sums)) * np.abs(c)
+
+    held, holes = np.argwhere(place >= 0), np.argwhere(place < 0)
+    for t, j in [held[i] for i in (0, len(held) // 3, len(held) // 2, 2 * len(held) // 3, len(held) - 1)] + [holes[len(holes) // 2]]:
+        up, down = w.clone(), w.clone()
+        up[t, j] += h; down[t, j] -= h
+        (a, ea), (b, eb) = loss(Y, up), loss(Y, down)
+        assert (np.delete(a, t, 0) == np.delete(b, t, 0)).all()         # the other tokens' rows: the same bits
+        if place[t, j] < 0:
+            assert (a == b).all() and float(dw[t, j]) == 0
+            continue
+        step = float(up[t, j].double() - down[t, j].double())
+        size = (np.abs(c[t]) * np.abs(Y[int(place[t, j])].double().cpu().numpy())).sum()
+        assert abs((a - b)[t].sum() / step - float(dw[t, j])) <= (ea + eb)[t].sum() / step + d * 2.0 ** -23 * size
+    for e in range(E):
+        r, col = int(offsets[e + 1]) - 1, (7 * e + 3) % d
+        assert r >= offsets[e]
+        up, down = Y.clone(), Y.clone()
+        up[r, col] += h; down[r, col] -= h
+        (a, ea), (b, eb) = loss(up, w), loss(down, w)
+        t = order[r] // K
+        step = float(up[r, col].double() - down[r, col].double())
+        assert step == 2 * h
+        grad = float(dY[r, col])
+        assert abs((a - b).sum() / step - grad) <= (ea + eb)[t, col] / step + 2 * (R.HALF_STEP[y_dtype] + 2.0 ** -24) * abs(grad)
 
 
 def test_gradient_of_the_dispatch():
