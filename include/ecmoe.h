@@ -346,8 +346,9 @@ ec_status ec_combine_backward(const ec_sort_config* cfg, const void* dX_out, con
  *                                           cols does not fill holds zeros (code 0) behind it
  *   scales [rows, ec_mx_scale_pitch(cols)]  a byte s per block; bytes behind the last block's are padding (written as 0 by the
  *                                           quantisation, never read by the product)
- * Matrices of several experts or batches follow one another.  Restrictions (EC_ERR_UNSUPPORTED): rows of a matrix in fp32 or bf16
- * a multiple of 16 bytes long; rows and columns <= 2^22 - 64 (rows of A: < 2^31 - 256); batches * rows < 2^31.
+ * Matrices of several experts or batches follow one another; outputs must not overlap inputs.  Restrictions
+ * (EC_ERR_UNSUPPORTED): rows of a matrix in fp32 or bf16 a multiple of 16 bytes long; rows and columns <= 2^22 - 64
+ * (rows of A: < 2^31 - 256); batches * rows < 2^31.
  */
 int64_t ec_mx_code_pitch(int64_t cols);   /* 16 * ceil(cols / 32); 0 if cols < 1 */
 int64_t ec_mx_scale_pitch(int64_t cols);  /* 16 * ceil(cols / 512); 0 if cols < 1 */

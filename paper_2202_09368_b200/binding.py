@@ -461,7 +461,8 @@ _ACTS = {"none": EC_MX_NONE, "erf": EC_MX_GELU_ERF, "tanh": EC_MX_GELU_TANH}
 def ec_mx_expert_gemm(A: Mx, W: Mx, offsets, bias=None, act="none", out=None, dtype=torch.bfloat16, ws=None):
     """act(A[r] . W[e]^T + bias[e]) for the rows offsets[e] <= r < offsets[e + 1]: A [rows, K], W [E, N, K].  out: a tensor [rows, N] (None:
     a new one of `dtype`) or an Mx to receive the result in the 4-bit format.  act: "none", "erf" or "tanh" (GeLU).  Rows of no
-    expert are left as they were."""
+    expert are left as they were.  ws: 256 bytes or more whose status word ec_read_status reads, the same for every product of a chain and
+    its plan; without it nobody can ask whether a wait ran out."""
     what = "ec_mx_expert_gemm"
     if A.codes.dim() != 2 or W.codes.dim() != 3 or act not in _ACTS:
         raise EcError(EC_ERR_INVALID_ARG, f"{what}: wanted A [rows, K], W [E, N, K] and an act of {tuple(_ACTS)}, got {A.codes.dim()} and {W.codes.dim()} axes, {act!r}")

@@ -19,9 +19,10 @@
 // MT = 2: two MMAs side by side, 256 columns of C, for long contractions (see wide()); the one accumulator's halves are handed over one by one
 // (32768 rows, 4096 x 16384, at the power cap: 1432 us, both at once 1471).
 // What bounds it: few rows, the reading of the weights (64 experts of 4096 x 16384, 32 rows each, 377 us, 92 % of the copy rate; eight rows of eight
-// experts 53 us, 82 %); many rows, the issuing warps and the 54 bytes a clock an SM receives from L2, then the board's 1000 W (32768 rows: 1190 us
-// alone, 1430 in a loop, 3.0 to 3.7 PFLOP/s); short contractions, the epilogue (16384 rows, 768 x 2048: 33 us, with GeLU 55, of which 17 are
-// the multiply-adds of the polynomial at full rate, to 4 bits 67).
+// experts 51 us, 84 %, of which 8 us do not grow with the experts: a call without rows takes 2, one with a single tile 10); many
+// rows, the issuing warps and the 54 bytes a clock an SM receives from L2, then the board's 1000 W (32768 rows: 1190 to 1330 us
+// alone, 1430 in a loop, 3.0 to 3.7 PFLOP/s); short contractions, the epilogue (16384 rows, 768 x 2048, bf16 results 31 us, with GeLU 53, of which
+// 17 are the multiply-adds of the polynomial at full rate; to 4 bits 46, with GeLU 65).
 // Two accumulators of NT columns, and as many buffers of scales as there are stages: a stage is full when its operands have landed and
 // its scales are in tensor memory, and one commit frees both.  (A wait that is over at once still takes the MMA warp 100 cycles, a commit
 // 60 to 100, issuing an MMA 80: with barriers of their own for the scales a stage took 815 cycles beside the MMAs' 384.)
@@ -659,7 +660,7 @@ cudaError_t launch_narrow(const MxGemmArgs& g, MxParams p, int sms, cudaStream_t
 }
 // 256 columns of C per tile instead of 128, where one accumulator for both halves leaves the epilogue in the open: a stage then takes 1028
 // cycles for two MMAs side by side instead of 775 for one (an SM receives 52 of its 54 bytes a clock with the narrow tiles, 56 KiB instead of
-// 80 for the same work here), the epilogue some 2700 per 128 columns, 5200 with GeLU, 7000 to 4 bits.  The fewest cycles for the
+// 80 for the same work here), the epilogue some 2700 per 128 columns, 5200 with GeLU, 7000 with it to 4 bits.  The fewest cycles for the
 // number of tiles to expect, an expert's last being half full.  Measured: 32768 rows, 64 experts, 4096 x 16384, at the power cap 1538 -> 1445 us;
 // 3062 rows, 16 experts, 4072 x 1096, 23.5 -> 19.2; 8192 x 4096 to 4 bits 175 -> 161; not taken: 2048 x 4096 53 and 66, 768 x 2048 33 and 45.
 bool wide(const MxGemmArgs& g, const MxParams& p, int sms) {

@@ -17,7 +17,7 @@ namespace {
 // Up to kOnePiece choices one CTA does it all, up to kClusterMost the eight of a cluster, which read each other's counts in shared
 // memory; beyond, a first launch leaves each piece's counts and, in `place`, ranks inside the piece, and in a second each CTA sums what it
 // needs of the counts (148 x 256 at most, 148 KiB out of L2) and adds.
-// Latency bounds it, its bytes being a few microseconds' at most: 128 choices 2.6 us, 2048 4.3, 16384 5.0 (two launches 6.4, one CTA 11), 32768 6.1
+// Latency bounds it, its bytes being a few microseconds' at most: 128 choices 2.7 us, 2048 4.4, 16384 5.2 (two launches 6.4, one CTA 11), 32768 7.1
 // (a cluster 7.5), 524288 of 256 experts 16.
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kMaxExperts = 256, kClusterCtas = 8;
 constexpr int64_t kOnePiece = 2048, kClusterMost = 24576;
