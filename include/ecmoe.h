@@ -300,8 +300,8 @@ ec_status ec_validate_routing(const ec_config* cfg, const int32_t* I, const int3
  * Row matrices (X_s, Y, dY) have n * per_token rows, of which the first m are read and written; the others are left as they were.
  * X, X_out, dX_out and X_s have the element type cfg->dtype, Y and dY cfg->y_dtype, weights and dweights are fp32.
  * Restrictions (EC_ERR_UNSUPPORTED): rows of d_model elements of either type a multiple of 16 bytes, d_model <= 2^22 - 64,
- * 1 <= E <= 256, 1 <= per_token <= 32, n * per_token < 2^31.  n = 0 is a call: it writes offsets (zeros) and
- * nothing else, and its empty arguments may be NULL.  An output must not overlap an input or another output.  Any contents of
+ * 1 <= E <= 256, 1 <= per_token <= 32, n * per_token < 2^31.  n = 0 is a call: it writes offsets (zeros) and no
+ * other array, and its empty arguments may be NULL.  An output must not overlap an input or another output.  Any contents of
  * `choice` and of `place` are safe to pass: what lies outside its range counts as "no expert".  ec_sort_tokens looks at its
  * arrays and its scratch and refuses those that overlap (EC_ERR_INVALID_ARG).
  */

@@ -8,7 +8,9 @@ namespace {
 
 inline bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 inline size_t esize(int dtype) { return dtype == EC_F32 ? 4 : 2; }
-inline bool overlap(const void* a, size_t na, const void* b, size_t nb) { return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na; }
+inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  return na > 0 && nb > 0 && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
 template <typename... P> bool bad_pointers(P... p) { return ((p == nullptr || misaligned(p, 16)) || ...); }
 // choice, offsets, order and place are read and written one by one: a slice of rows, or one layer of a stack, need not begin at 16 bytes
 template <typename... P> bool bad_indices(const P*... p) { return ((p == nullptr || misaligned(p, 4)) || ...); }
@@ -37,13 +39,12 @@ ec_status ec_sort_tokens(const ec_sort_config* c, const int32_t* choice, int32_t
   if (bad_indices(offsets) || ws == nullptr || misaligned(ws, 256)) return EC_ERR_INVALID_ARG;
   if (c->n > 0 && bad_indices(choice, order, place)) return EC_ERR_INVALID_ARG;
   if (ws_bytes < ec_sort_workspace_bytes(c)) return EC_ERR_WORKSPACE;
-  if (c->n > 0) {      // the kernels index by what they read back of these arrays
-    const size_t flat = (size_t)(c->n * c->per_token) * 4;
-    const void* at[] = {choice, offsets, order, place, ws};
-    const size_t bytes[] = {flat, (size_t)(c->E + 1) * 4, flat, flat, sort_scratch_bytes(c->E)};
-    for (int i = 0; i < 5; ++i)
-      for (int j = 0; j < i; ++j) if (overlap(at[i], bytes[i], at[j], bytes[j])) return EC_ERR_INVALID_ARG;
-  }
+  // the kernels index by what they read back of these arrays
+  const size_t flat = (size_t)(c->n * c->per_token) * 4;
+  const void* at[] = {choice, offsets, order, place, ws};
+  const size_t bytes[] = {flat, (size_t)(c->E + 1) * 4, flat, flat, sort_scratch_bytes(c->E)};
+  for (int i = 0; i < 5; ++i)
+    for (int j = 0; j < i; ++j) if (overlap(at[i], bytes[i], at[j], bytes[j])) return EC_ERR_INVALID_ARG;
   EC_CUDA(launch_sort_tokens(choice, c->n * c->per_token, c->E, offsets, order, place, ws, (cudaStream_t)stream));
   return EC_OK;
 }

@@ -94,6 +94,13 @@ def test_no_tokens():
             L.ec_combine_backward(r, None, None, None, None, None, None, None)] == [B.EC_OK] * 3
 
 
+def test_no_tokens_and_offsets_on_the_workspace():
+    """The plan of no tokens writes its offsets and the status word: not on one another."""
+    cfg, L = B.make_sort_config(0, 64, 8, 2), B.lib()
+    for ws in (4096, 4096 - 256):
+        assert L.ec_sort_tokens(C.byref(cfg), None, 4096 + 16, None, None, ws, 1 << 18, None) == B.EC_ERR_INVALID_ARG
+
+
 def test_tensors_that_are_not_the_current_device_s():
     cfg = B.make_sort_config(16, 64, 8, 2)
     x, p = torch.zeros(16, 64), torch.zeros(16, 2, dtype=torch.int32)
